@@ -268,6 +268,77 @@ lvx_status_t lvx_layernorm_modulate(const void *dev_x, int64_t ldx, const float 
                                     float eps, int32_t n_tokens, int32_t d, void *dev_u, int64_t ldu, lvx_stream_t stream);
 
 /* ------------------------------------------------------------------------------------------------
+ * Decoder layers of a language model on the same card, with weights and cache in 4 bits (E2M1: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and
+ * their negatives, which the matrix cores take).  A layer: lvx_rmsnorm_residual_fp8 -> lvx_linear_fp8_fp4 (q | k | v) -> lvx_kv4_append ->
+ * lvx_kv4_attention -> lvx_linear_fp4 with the residual, and the same around the feed-forward pair.  Lengths and row ranges that change
+ * from step to step are device arrays, so that a captured step replays with other lengths.
+ * ------------------------------------------------------------------------------------------------ */
+
+/* h = x + resid;  y = h / sqrt(mean_c(h^2) + eps) * gain,  fp32 throughout; the norm sees h un-rounded.
+ *   x bf16 or NULL (0); resid bf16, or fp32 with resid_is_f32 = 1 (strides in fp32 elements), or NULL (0), not both NULL; gain fp32 [d] or NULL (1).
+ *   dev_sum (may be NULL; needs a residual): h in the residual's type.  dev_y: bf16.  Each output may be the buffer of an input of the same type
+ *   and stride.  d % 8 == 0, d <= 16384, strides % 8 == 0.
+ * lvx_rmsnorm_residual_fp8: y leaves as E4M3 codes with one fp32 scale a row: scale = max|y| / 448 (1 for a zero row), code =
+ *   E4M3(y * (448 / max|y|)), nearest-even: what lvx_linear_fp8_fp4 takes.  d % 16 == 0, ldq % 16 == 0.  A row that holds a NaN or an
+ *   infinity has a NaN scale. */
+lvx_status_t lvx_rmsnorm_residual(const void *dev_x, int64_t ldx, const void *dev_resid, int64_t ldr, int32_t resid_is_f32, const float *dev_gain,
+                                  float eps, int32_t n_tokens, int32_t d, void *dev_sum, int64_t ld_sum, void *dev_y, int64_t ldy,
+                                  lvx_stream_t stream);
+lvx_status_t lvx_rmsnorm_residual_fp8(const void *dev_x, int64_t ldx, const void *dev_resid, int64_t ldr, int32_t resid_is_f32, const float *dev_gain,
+                                      float eps, int32_t n_tokens, int32_t d, void *dev_sum, int64_t ld_sum, void *dev_q, int64_t ldq,
+                                      float *dev_row_scales, lvx_stream_t stream);
+
+/* bf16 [rows][ld] -> E2M1 codes [rows][ldq bytes], two to a byte with the even column in the low half, and one E8M0 byte (2^(byte - 127)) per 32
+ * columns, [rows][lds bytes]: the smallest exponent >= -120 with max|x| <= 7 * 2^e; nearest, ties to the even code, saturating at 6.  A group that holds
+ * a NaN or an infinity gets scale 255 (NaN).  cols % 32 == 0, ldq >= cols / 2 and % 16 == 0, lds >= cols / 32.  For weights, once. */
+lvx_status_t lvx_fp4_quantize(const void *dev_x, int64_t ld, int32_t rows, int32_t cols, void *dev_q, int64_t ldq, void *dev_scales, int64_t lds,
+                              lvx_stream_t stream);
+/* C[M][N] = epilogue(A[M][K] * W[N][K]^T), W in that form (any scale byte; 255 is NaN), fp32 accumulate; for one row as for a prompt.
+ *   lvx_linear_fp4: A bf16, lda % 8 == 0.   lvx_linear_fp8_fp4: A E4M3 codes with a scale per row, lda in bytes % 16 == 0.
+ * K % 32 == 0, N % 8 == 0, ldc, ldr % 8 == 0, ldw in bytes % 16 == 0.  Epilogues STORE, GELU_TANH, RESID_GATE, RESID_GATE_F32, STORE_F32; C may alias R.
+ * The same call gives the same bits; the order of summation depends on M, N and K. */
+lvx_status_t lvx_linear_fp4(const void *dev_a, int64_t lda, const void *dev_wq, int64_t ldw, const void *dev_w_scales, int64_t lds, void *dev_c,
+                            int64_t ldc, int32_t M, int32_t N, int32_t K, lvx_epilogue_t epi, const void *dev_resid, int64_t ldr,
+                            const float *dev_gate, lvx_stream_t stream);
+lvx_status_t lvx_linear_fp8_fp4(const void *dev_aq, int64_t lda, const float *dev_row_scales, const void *dev_wq, int64_t ldw,
+                                const void *dev_w_scales, int64_t lds, void *dev_c, int64_t ldc, int32_t M, int32_t N, int32_t K,
+                                lvx_epilogue_t epi, const void *dev_resid, int64_t ldr, const float *dev_gate, lvx_stream_t stream);
+
+/* KV cache in 4 bits for n_seqs sequences, grouped heads: head h of the queries reads kv head h / (n_heads / n_kv_heads).  Keys: E2M1 codes with an E8M0
+ * scale per key and 32 channels, as lvx_fp4_quantize makes them.  Values: E2M1 codes with one bf16 scale s per key and head, s = bf16(max|v| / 6),
+ * at least 2^-120, code = E2M1(v / s).  132 .. 134 bytes per key and kv head of 128 channels.  Storage (caller-owned, 256-byte aligned, alive as long as
+ * the handle) need not be cleared; its layout is private.
+ *
+ * A call handles n_tokens new tokens in all, at most max_tokens of a sequence: sequence s has rows [dev_starts[s], dev_starts[s + 1]) (device int32 [n_seqs + 1];
+ * NULL: max_tokens rows each, n_tokens = n_seqs * max_tokens), and dev_key_counts[s] (device int32 [n_seqs]) keys with its new tokens, so that its token i of n
+ * is key dev_key_counts[s] - n + i.  Idle sequences have no rows.  Rows behind the last sequence are neither read nor written.  Counts beyond max_keys count
+ * as max_keys; row ranges are cut to [0, n_tokens).
+ *   lvx_kv4_append     quantises the new tokens' k and v ([n_tokens][ld], kv head h at columns h * head_dim) into their places; a place outside [0, max_keys) is not written.
+ *   lvx_kv4_gather     keys [first_key, first_key + n_keys) of all sequences of a layer back as bf16 [n_seqs][n_keys][ld] (keys exact, values code * s rounded once); zeros
+ *                      from a sequence's key count on.
+ *   lvx_kv4_attention  o = sum_j softmax_j(scale * q.k_j) v_j.  causal = 1: token i of n sees the keys up to its own, dev_key_counts[s] - (n - 1 - i) of them; 0: every
+ *                      token sees dev_key_counts[s].  A token that sees no key gets zeros.  q, out: [n_tokens][ld] bf16, head h at columns h * head_dim;
+ *                      out may be the buffer of q.  fp32 softmax; probability times value scale rounded to bf16 once.  The same call gives the same bits;
+ *                      the order of summation depends on the descriptor, n_heads, max_tokens and the key counts.
+ *                      dev_workspace: lvx_kv4_attention_workspace_bytes(cache, n_heads, max_tokens) bytes, 16-byte aligned, not shared by calls that may overlap.
+ * Errors: INVALID_ARG, SHAPE, UNSUPPORTED (head_dim not 64 or 128). */
+typedef struct {
+    int32_t n_layers, n_seqs, n_kv_heads, head_dim, max_keys;
+} lvx_kv4_desc_t;
+typedef struct lvx_kv4 lvx_kv4_t; /* opaque host-side handle */
+size_t lvx_kv4_bytes(const lvx_kv4_desc_t *desc /* host */);
+lvx_status_t lvx_kv4_init(const lvx_kv4_desc_t *desc /* host */, void *dev_storage, size_t bytes, lvx_kv4_t **out /* host */);
+lvx_status_t lvx_kv4_destroy(lvx_kv4_t *cache);
+lvx_status_t lvx_kv4_append(lvx_kv4_t *cache, int32_t layer, const void *dev_k, const void *dev_v, int64_t ld, const int32_t *dev_starts,
+                            int32_t n_tokens, int32_t max_tokens, const int32_t *dev_key_counts, lvx_stream_t stream);
+lvx_status_t lvx_kv4_gather(const lvx_kv4_t *cache, int32_t layer, int32_t first_key, int32_t n_keys, const int32_t *dev_key_counts, void *dev_k_out,
+                            void *dev_v_out, int64_t ld, lvx_stream_t stream);
+size_t lvx_kv4_attention_workspace_bytes(const lvx_kv4_t *cache, int32_t n_heads, int32_t max_tokens);
+lvx_status_t lvx_kv4_attention(const lvx_kv4_t *cache, int32_t layer, const void *dev_q, int64_t ld_q, int32_t n_heads, const int32_t *dev_starts,
+                               int32_t n_tokens, int32_t max_tokens, const int32_t *dev_key_counts, int32_t causal, float scale, void *dev_out,
+                               int64_t ld_out, void *dev_workspace, size_t workspace_bytes, lvx_stream_t stream);
+
+/* ------------------------------------------------------------------------------------------------
  * DiT block and denoise stage (Alg. 4, DiT-device branch: forward with the local rolling cache, cache update,
  * Euler step x <- x + v dt).  Block wiring (the paper defers to its base architecture; this is the workload's):
  *   u  = LN(x)(1+scale1)+shift1;  [q|k|v] = u W_qkv^T;  q^,k^ = RoPE(RMSNorm(q,k));  append(k^, v);

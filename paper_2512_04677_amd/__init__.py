@@ -52,6 +52,10 @@ class ConvDesc(C.Structure):
     _fields_ = [("c_in", C.c_int32), ("c_out", C.c_int32), ("height", C.c_int32), ("width", C.c_int32), ("max_frames", C.c_int32)]
 
 
+class KV4Desc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_layers", "n_seqs", "n_kv_heads", "head_dim", "max_keys")]
+
+
 class BlockWeightsFp8(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("W_qkv", "W_o", "Wc_q", "Wc_k", "Wc_v", "Wc_o", "W_1", "W_2", "scales")]
 
@@ -89,6 +93,18 @@ SIGNATURES = {
     "lvx_fp8_quantize_static": (C.c_int, [_vp, _i64, _i32, _i32, _vp, _i64, _vp, _vp]),
     "lvx_linear_fp8": (C.c_int, [_vp, _i64, _vp, _vp, _i64, _vp, _vp, _i64, _i32, _i32, _i32, C.c_int, _vp, _i64, _vp, _vp]),
     "lvx_layernorm_modulate": (C.c_int, [_vp, _i64, _vp, _vp, _f32, _i32, _i32, _vp, _i64, _vp]),
+    "lvx_rmsnorm_residual": (C.c_int, [_vp, _i64, _vp, _i64, _i32, _vp, _f32, _i32, _i32, _vp, _i64, _vp, _i64, _vp]),
+    "lvx_rmsnorm_residual_fp8": (C.c_int, [_vp, _i64, _vp, _i64, _i32, _vp, _f32, _i32, _i32, _vp, _i64, _vp, _i64, _vp, _vp]),
+    "lvx_fp4_quantize": (C.c_int, [_vp, _i64, _i32, _i32, _vp, _i64, _vp, _i64, _vp]),
+    "lvx_linear_fp4": (C.c_int, [_vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _i32, _i32, _i32, C.c_int, _vp, _i64, _vp, _vp]),
+    "lvx_linear_fp8_fp4": (C.c_int, [_vp, _i64, _vp, _vp, _i64, _vp, _i64, _vp, _i64, _i32, _i32, _i32, C.c_int, _vp, _i64, _vp, _vp]),
+    "lvx_kv4_bytes": (_sz, [C.POINTER(KV4Desc)]),
+    "lvx_kv4_init": (C.c_int, [C.POINTER(KV4Desc), _vp, _sz, C.POINTER(_vp)]),
+    "lvx_kv4_destroy": (C.c_int, [_vp]),
+    "lvx_kv4_append": (C.c_int, [_vp, _i32, _vp, _vp, _i64, _vp, _i32, _i32, _vp, _vp]),
+    "lvx_kv4_gather": (C.c_int, [_vp, _i32, _i32, _i32, _vp, _vp, _vp, _i64, _vp]),
+    "lvx_kv4_attention_workspace_bytes": (_sz, [_vp, _i32, _i32]),
+    "lvx_kv4_attention": (C.c_int, [_vp, _i32, _vp, _i64, _i32, _vp, _i32, _i32, _vp, _i32, _f32, _vp, _i64, _vp, _sz, _vp]),
     "lvx_workspace_bytes": (_sz, [C.POINTER(Stage), _i32, _i32]),
     "lvx_context_kv": (C.c_int, [C.POINTER(Stage), _i32, _i32, _vp, _i32, _vp, _vp, _i64, _vp, _sz, _vp]),
     "lvx_dit_block": (C.c_int, [C.POINTER(Stage), _i32, _vp, _vp, _i32, _vp, _i32, _vp, _i64, _i32, _vp, _sz, _vp]),
@@ -319,6 +335,117 @@ def lvx_linear_fp8(aq, scale_a, wq, scale_w, c, epi=EPI_STORE, resid=None, gate=
 def lvx_layernorm_modulate(x, shift, scale, eps, u):
     _check(load().lvx_layernorm_modulate(_ptr(x), x.stride(0), _ptr(shift), _ptr(scale), eps, x.shape[0], x.shape[1],
                                          _ptr(u), u.stride(0), _stream()))
+
+
+def _norm_args(x, resid, gain, eps, sum_out):
+    import torch
+    ref = x if x is not None else resid
+    return (_ptr(x), x.stride(0) if x is not None else 0, _ptr(resid), resid.stride(0) if resid is not None else 0,
+            1 if resid is not None and resid.dtype == torch.float32 else 0, _ptr(gain), eps, ref.shape[0], ref.shape[1], _ptr(sum_out),
+            sum_out.stride(0) if sum_out is not None else 0)
+
+
+def lvx_rmsnorm_residual(x, resid, gain, eps, y, sum_out=None):
+    """y = RMSNorm(x + resid) * gain in bf16; sum_out (the residual's dtype) receives x + resid.  x or resid may be None."""
+    _check_like(resid, sum_out)
+    _check(load().lvx_rmsnorm_residual(*_norm_args(x, resid, gain, eps, sum_out), _ptr(y), y.stride(0), _stream()))
+
+
+def lvx_rmsnorm_residual_fp8(x, resid, gain, eps, q, row_scales, sum_out=None):
+    """The same with y as E4M3 codes (uint8 [n][>= d]) and one fp32 scale a row."""
+    _check_like(resid, sum_out)
+    _check(load().lvx_rmsnorm_residual_fp8(*_norm_args(x, resid, gain, eps, sum_out), _ptr(q), q.stride(0), _ptr(row_scales), _stream()))
+
+
+def _check_like(resid, sum_out):
+    if sum_out is not None and (resid is None or sum_out.dtype != resid.dtype):
+        raise LvxError(1, "the sum has the residual's dtype")
+
+
+def lvx_fp4_quantize(x, q=None, scales=None):
+    """bf16 [rows][cols] -> (E2M1 codes uint8 [rows][cols / 2], E8M0 scales uint8 [rows][cols / 32])."""
+    import torch
+    rows, cols = x.shape
+    if q is None:
+        q = torch.empty((rows, cols // 2), dtype=torch.uint8, device=x.device)
+    if scales is None:
+        scales = torch.empty((rows, cols // 32), dtype=torch.uint8, device=x.device)
+    _check(load().lvx_fp4_quantize(_ptr(x), x.stride(0), rows, cols, _ptr(q), q.stride(0), _ptr(scales), scales.stride(0), _stream()))
+    return q, scales
+
+
+def lvx_linear_fp4(a, wq, w_scales, c, epi=EPI_STORE, resid=None, gate=None):
+    """c = epilogue(a [M][K] bf16 times the E2M1 weights wq [N][K / 2] with scales [N][K / 32], transposed)."""
+    _check(load().lvx_linear_fp4(_ptr(a), a.stride(0), _ptr(wq), wq.stride(0), _ptr(w_scales), w_scales.stride(0), _ptr(c), c.stride(0), a.shape[0],
+                                 wq.shape[0], a.shape[1], epi, _ptr(resid), resid.stride(0) if resid is not None else 0, _ptr(gate), _stream()))
+
+
+def lvx_linear_fp8_fp4(aq, row_scales, wq, w_scales, c, epi=EPI_STORE, resid=None, gate=None):
+    """The same for E4M3 rows (uint8 [M][K]) with one fp32 scale each."""
+    _check(load().lvx_linear_fp8_fp4(_ptr(aq), aq.stride(0), _ptr(row_scales), _ptr(wq), wq.stride(0), _ptr(w_scales), w_scales.stride(0), _ptr(c),
+                                     c.stride(0), aq.shape[0], wq.shape[0], aq.shape[1], epi, _ptr(resid), resid.stride(0) if resid is not None else 0,
+                                     _ptr(gate), _stream()))
+
+
+def kv4_desc(n_layers, n_seqs, n_kv_heads, head_dim, max_keys):
+    return KV4Desc(n_layers, n_seqs, n_kv_heads, head_dim, max_keys)
+
+
+class KV4Cache:
+    """Owns the torch storage tensor and the library handle of one 4-bit cache."""
+
+    def __init__(self, desc, device="cuda:0"):
+        import torch
+        self.desc = desc
+        self.handle = None
+        nbytes = load().lvx_kv4_bytes(C.byref(desc))
+        if nbytes == 0:
+            raise LvxError(2, load().lvx_last_error().decode())
+        self.storage = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        h = C.c_void_p()
+        _check(load().lvx_kv4_init(C.byref(desc), _ptr(self.storage), nbytes, C.byref(h)))
+        self.handle = h
+
+    def close(self):
+        if self.handle is not None:
+            load().lvx_kv4_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def lvx_kv4_append(cache, layer, k, v, key_counts, starts=None, max_tokens=1, n_tokens=None):
+    """k, v: bf16 [n_tokens][kv heads * head_dim] of one row stride; key_counts, starts: device int32."""
+    if k.stride(0) != v.stride(0):
+        raise LvxError(2, "k and v must share their row stride")
+    _check(load().lvx_kv4_append(cache.handle, layer, _ptr(k), _ptr(v), k.stride(0), _ptr(starts), k.shape[0] if n_tokens is None else n_tokens, max_tokens,
+                                 _ptr(key_counts), _stream()))
+
+
+def lvx_kv4_gather(cache, layer, key_counts, k_out, v_out, first_key=0):
+    """k_out, v_out: bf16 [n_seqs][n_keys][kv heads * head_dim], contiguous but for a padded row, of the same strides."""
+    for t in (k_out, v_out):
+        if t.dim() != 3 or t.shape[0] != cache.desc.n_seqs or t.stride() != k_out.stride() or t.stride(0) != t.shape[1] * t.stride(1):
+            raise LvxError(2, "the outputs are [n_seqs][n_keys][columns] of the same strides")
+    _check(load().lvx_kv4_gather(cache.handle, layer, first_key, k_out.shape[1], _ptr(key_counts), _ptr(k_out), _ptr(v_out), k_out.stride(1), _stream()))
+
+
+def lvx_kv4_attention_workspace_bytes(cache, n_heads, max_tokens):
+    n = load().lvx_kv4_attention_workspace_bytes(cache.handle, n_heads, max_tokens)
+    if n == 0:
+        raise LvxError(1, load().lvx_last_error().decode())
+    return n
+
+
+def lvx_kv4_attention(cache, layer, q, n_heads, scale, key_counts, out, workspace, starts=None, max_tokens=1, causal=True, n_tokens=None):
+    """q, out: bf16 [n_tokens][heads * head_dim]; workspace: lvx_kv4_attention_workspace_bytes(cache, n_heads, max_tokens) bytes."""
+    _check(load().lvx_kv4_attention(cache.handle, layer, _ptr(q), q.stride(0), n_heads, _ptr(starts), q.shape[0] if n_tokens is None else n_tokens, max_tokens,
+                                    _ptr(key_counts), 1 if causal else 0, scale, _ptr(out), out.stride(0), _ptr(workspace),
+                                    workspace.numel() * workspace.element_size(), _stream()))
 
 
 class StageHandle:

@@ -1,0 +1,146 @@
+"""4-bit quantisation (bit for bit) and the linears with 4-bit weights against the 64-bit oracle.
+
+Tolerance of a product: every term is exact in fp32 or its operands are, and K terms are added in fp32 in some order, so the sum is off by at most
+(K + 8) * 2^-24 * sum_k |a w|; a bf16 output by half a step (2^-8 of itself) more.  GELU is 1.13-Lipschitz and its own fp32 evaluation is off by at most
+2^-18 of |x| (its exponential's argument reaches tens)."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import lvx_synth as S
+from oracle import decoder_oracle as O
+from oracle.lvx_oracle import gelu_tanh
+from test_gpu_fp8 import e4m3_decode
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def unpack(q):
+    q = q.cpu().numpy()
+    return np.stack([q & 15, q >> 4], -1).reshape(q.shape[0], -1)
+
+
+@pytest.mark.parametrize("rows,cols,std", [(5, 32, 1.0), (37, 96, 0.02), (1, 4096, 30.0), (130, 160, 1e-3)])
+def test_quantize_codes_and_scales(lvx, rows, cols, std):
+    x = S.randn_bf16((rows, cols + 8), S.seed_of("fp4q", rows, cols), std, device=DEV)[:, :cols].clone()
+    pad = torch.empty(rows, cols + 8, dtype=torch.bfloat16, device=DEV)
+    x[0, :32] = 0
+    x[rows // 2, 3] = 7.0 * 2.0 ** 20                       # exactly at the border of a scale
+    x[rows - 1, 1] = 7.0625
+    x[0, cols - 1] = -0.0
+    pad[:, :cols] = x
+    q = torch.full((rows + 1, -(-(cols // 2) // 16) * 16 + 16), 0x5a, dtype=torch.uint8, device=DEV)
+    s = torch.full((rows + 1, cols // 32 + 3), 0x5a, dtype=torch.uint8, device=DEV)
+    lvx.lvx_fp4_quantize(pad[:, :cols], q[:rows, :cols // 2], s[:rows, :cols // 32])
+    code, e, _ = O.quantise_groups(S.to_f64(x))
+    got = unpack(q[:rows, :cols // 2])
+    zero = O.LEVELS[code & 7] == 0                           # the sign of a zero is kept, too
+    assert np.array_equal(got, code) and zero.any()
+    assert np.array_equal(s[:rows, :cols // 32].cpu().numpy().astype(np.int64) - 127, e)
+    assert bool((q[rows] == 0x5a).all()) and bool((q[:, cols // 2:] == 0x5a).all()) and bool((s[rows] == 0x5a).all()) and bool((s[:, cols // 32:] == 0x5a).all())
+
+
+def test_quantize_non_finite_groups(lvx):
+    x = torch.ones(2, 96, dtype=torch.bfloat16, device=DEV)
+    x[0, 40], x[1, 95] = float("nan"), float("-inf")
+    q, s = lvx.lvx_fp4_quantize(x)
+    s = s.cpu().numpy()
+    assert s[0, 1] == 255 and s[1, 2] == 255 and (s != 255).sum() == 4
+    # every such group makes NaN of the outputs that read it
+    c = torch.zeros(1, 8, device=DEV)
+    w, ws = q[:1].repeat(8, 1), torch.tensor(s[:1], device=DEV).repeat(8, 1)
+    ws[4:] = 127
+    for m in (1, 70):
+        c = torch.zeros(m, 8, device=DEV)
+        lvx.lvx_linear_fp4(torch.ones(m, 96, dtype=torch.bfloat16, device=DEV), w, ws, c, lvx.EPI_STORE_F32)
+        assert bool(torch.isnan(c[:, :4]).all()) and bool(torch.isfinite(c[:, 4:]).all())
+
+
+def weights(lvx, N, K, tag):
+    w = S.randn_bf16((N, K), S.seed_of(tag, "w", N, K), 1 / math.sqrt(K), device=DEV) * torch.exp2(torch.randint(-3, 4, (N, 1), device=DEV).float()).to(torch.bfloat16)
+    q, s = lvx.lvx_fp4_quantize(w)
+    codes = unpack(q)
+    return q, s, (O.e2m1_value(codes).reshape(N, -1, 32) * np.exp2(s.cpu().numpy().astype(np.float64) - 127)[..., None]).reshape(N, K)
+
+
+def rows8(M, K, tag):
+    """E4M3 codes without NaN, some of them subnormal, and a scale per row."""
+    c = S.randn_f32((M, K), S.seed_of(tag, "a8", M, K), 60.0, device=DEV).to(torch.float8_e4m3fn).view(torch.uint8).clone()
+    c[:, ::7] &= 0x83
+    s = torch.exp(S.randn_f32((M,), S.seed_of(tag, "s8", M), 1.0, device=DEV)) / 448
+    return c, s, e4m3_decode(c.cpu().numpy()) * S.to_f64(s)[:, None]
+
+
+def products(lvx, M, N, K, a8, tag):
+    q, s, w = weights(lvx, N, K, tag)
+    if a8:
+        c, sa, a = rows8(M, K, tag)
+        call = lambda out, *x, **k: lvx.lvx_linear_fp8_fp4(c, sa, q, s, out, *x, **k)
+    else:
+        x = S.randn_bf16((M, K + 8), S.seed_of(tag, "a", M, K), 1.0, device=DEV)[:, :K]
+        a = S.to_f64(x)
+        call = lambda out, *z, **k: lvx.lvx_linear_fp4(x, q, s, out, *z, **k)
+    return call, a @ w.T, (K + 8) * 2.0 ** -24 * (np.abs(a) @ np.abs(w).T)
+
+
+SHAPES = [(1, 8, 32), (1, 264, 5120), (2, 40, 96), (15, 72, 160), (16, 520, 1184), (17, 64, 224), (31, 8, 4096), (33, 136, 128), (48, 1032, 608),
+          (64, 256, 64), (65, 24, 352), (100, 392, 1120), (129, 128, 512), (257, 648, 288), (544, 1288, 416)]
+
+
+@pytest.mark.parametrize("a8", [False, True])
+@pytest.mark.parametrize("M,N,K", SHAPES)
+def test_linear(lvx, M, N, K, a8):
+    call, ref, off = products(lvx, M, N, K, a8, "lin")
+    out = torch.full((M + 1, N + 8), 7.0, dtype=torch.bfloat16, device=DEV)
+    call(out[:M, :N])
+    assert np.all(np.abs(S.to_f64(out[:M, :N]) - ref) <= 2.0 ** -8 * np.abs(ref) + 2 * off)
+    assert bool((out[M:] == 7).all()) and bool((out[:, N:] == 7).all())
+    again = torch.empty_like(out)
+    call(again[:M, :N])
+    assert torch.equal(again[:M, :N], out[:M, :N])
+    o32 = torch.full((M + 1, N + 8), 7.0, device=DEV)
+    call(o32[:M, :N], lvx.EPI_STORE_F32)
+    assert np.all(np.abs(S.to_f64(o32[:M, :N]) - ref) <= off)
+    assert bool((o32[M:] == 7).all()) and bool((o32[:, N:] == 7).all())
+
+
+@pytest.mark.parametrize("a8", [False, True])
+@pytest.mark.parametrize("M,N,K", [(1, 72, 288), (20, 264, 512), (150, 136, 160)])
+def test_linear_epilogues(lvx, M, N, K, a8):
+    call, ref, off = products(lvx, M, N, K, a8, "epi")
+    out = torch.empty(M, N, dtype=torch.bfloat16, device=DEV)
+    call(out, lvx.EPI_GELU_TANH)
+    want = gelu_tanh(ref)
+    assert np.all(np.abs(S.to_f64(out) - want) <= 2.0 ** -8 * np.abs(want) + 2 * off + 2.0 ** -18 * np.abs(ref))
+    r = S.randn_bf16((M, N), S.seed_of("epi_r", M, N), 2.0, device=DEV)
+    g = S.randn_f32((N,), S.seed_of("epi_g", N), 1.0, device=DEV)
+    for gate in (None, g):
+        gg = 1.0 if gate is None else S.to_f64(gate)
+        want = S.to_f64(r) + gg * ref
+        slack = 2 * (off * np.abs(gg) + 2.0 ** -24 * np.abs(gg * ref))
+        c = r.clone()
+        call(c, lvx.EPI_RESID_GATE, resid=c, gate=gate)     # in place
+        assert np.all(np.abs(S.to_f64(c) - want) <= 2.0 ** -8 * np.abs(want) + slack)
+        c = r.float()
+        call(c, lvx.EPI_RESID_GATE_F32, resid=c, gate=gate)
+        assert np.all(np.abs(S.to_f64(c) - want) <= 2.0 ** -24 * np.abs(want) + slack)
+
+
+def test_linear_scale_extremes_and_neighbours(lvx):
+    """Scale bytes from 2^-100 to 2^100 a row; a NaN in one activation row stays in it."""
+    M, N, K = 18, 32, 256
+    q, s, w = weights(lvx, N, K, "ext")
+    s = torch.randint(27, 228, (N, 1), dtype=torch.uint8, device=DEV).repeat(1, K // 32)
+    codes = unpack(q)
+    w = (O.e2m1_value(codes).reshape(N, -1, 32) * np.exp2(s.cpu().numpy().astype(np.float64) - 127)[..., None]).reshape(N, K)
+    a = S.randn_bf16((M, K), S.seed_of("ext_a"), 1.0, device=DEV).clone()
+    a[3, 100] = float("nan")
+    c = torch.empty(M, N, device=DEV)
+    lvx.lvx_linear_fp4(a, q, s, c, lvx.EPI_STORE_F32)
+    keep = [m for m in range(M) if m != 3]
+    x = S.to_f64(a)[keep]
+    assert np.all(np.abs(S.to_f64(c)[keep] - x @ w.T) <= (K + 8) * 2.0 ** -24 * (np.abs(x) @ np.abs(w).T))
+    assert bool(torch.isnan(c[3]).all())
