@@ -26,91 +26,87 @@ __device__ __forceinline__ bf16x8_t fp8x8_bf16(uint32_t lo, uint32_t hi) {
     return r;
 }
 
-// four consecutive columns n .. n + 3 of row m
-__device__ __forceinline__ void fp4_store(const fp4_args_t &p, int m, int n, f32x4_t c) {
-    float v[4] = {c[0], c[1], c[2], c[3]};
-    if (p.row_scales != nullptr) {
-        const float s = p.row_scales[m];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] *= s;
-    }
-    if (p.epi == LVX_EPI_GELU_TANH) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = gelu_tanh_f32(v[i]);
-    } else if (p.epi == LVX_EPI_RESID_GATE || p.epi == LVX_EPI_RESID_GATE_F32) {
-        if (p.gate != nullptr) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] *= p.gate[n + i];
-        }
-        if (p.epi == LVX_EPI_RESID_GATE) {
-            const uint2 r = *reinterpret_cast<const uint2 *>((const bf16_t *)p.R + m * p.ldr + n);
-            v[0] += bf16_lo(r.x), v[1] += bf16_hi(r.x), v[2] += bf16_lo(r.y), v[3] += bf16_hi(r.y);
-        } else {
-            const float4 r = *reinterpret_cast<const float4 *>((const float *)p.R + m * p.ldr + n);
-            v[0] += r.x, v[1] += r.y, v[2] += r.z, v[3] += r.w;
-        }
-    }
-    if (p.epi == LVX_EPI_RESID_GATE_F32 || p.epi == LVX_EPI_STORE_F32)
-        *reinterpret_cast<float4 *>((float *)p.C + m * p.ldc + n) = make_float4(v[0], v[1], v[2], v[3]);
-    else
-        *reinterpret_cast<uint2 *>((bf16_t *)p.C + m * p.ldc + n) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
-}
-
-// A workgroup of KW waves owns 16 NB columns and 16 MB rows of C; its waves take every KW-th step of 128 channels.
-template <int MB, int NB, int KW, bool A8>
-__global__ void __launch_bounds__(64 * KW) lvx_fp4_linear_kernel(fp4_args_t p) {
-    __shared__ f32x4_t part[KW][NB * MB][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int r = lane & 15, g = lane >> 4;
-    const int n0 = blockIdx.x * 16 * NB, m0 = blockIdx.y * 16 * MB;
-    const uint8_t *w_row[NB], *s_row[NB];
-    const char *a_row[MB];
-    // rows and columns past the end repeat the last one: they are read, multiplied and not stored
-#pragma unroll
-    for (int b = 0; b < NB; ++b) {
-        const int n = n0 + 16 * b + r < p.N ? n0 + 16 * b + r : p.N - 1;
-        w_row[b] = p.W + n * p.ldw + 16 * g;
-        s_row[b] = p.S + n * p.lds + g;
-    }
-#pragma unroll
-    for (int b = 0; b < MB; ++b) {
-        const int m = m0 + 16 * b + r < p.M ? m0 + 16 * b + r : p.M - 1;
-        a_row[b] = p.A + m * p.lda + (A8 ? 32 : 64) * g;
-    }
-    f32x4_t acc[NB][MB];
-#pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-        for (int c = 0; c < MB; ++c) acc[b][c] = {0, 0, 0, 0};
-
-    const int steps = (p.K + 127) / 128;
-    for (int t = wave; t < steps; t += KW) {
-        const bool in = 128 * t + 32 * g < p.K;  // the last step may hold one to three groups of 32 channels
-        uint4 w[NB];
-        float s[NB];
-#pragma unroll
-        for (int b = 0; b < NB; ++b) {
-            w[b] = in ? *reinterpret_cast<const uint4 *>(w_row[b] + (size_t)64 * t) : make_uint4(0, 0, 0, 0);
-            s[b] = in ? lvx_e8m0_f32(s_row[b][(size_t)4 * t]) : 1.0f;
-        }
-        bf16x8_t a[MB][4];
+// Blocks of 16 columns and MB blocks of 16 rows: a lane has columns n .. n + 3 of row m0 + 16 c + lane % 16.  Everything that is read is requested before the first
+// store: the compiler moves no load past a store that may alias it, and each would be waited for in turn.
+template <int MB>
+__device__ __forceinline__ void fp4_store(const fp4_args_t &p, int m0, int n, const f32x4_t (&acc)[MB], const float (&row_scale)[MB]) {
+    if (n >= p.N) return;
+    float4 gate = make_float4(1.f, 1.f, 1.f, 1.f);
+    float4 r32[MB];
+    uint2 r16[MB];
+    if (p.epi == LVX_EPI_RESID_GATE || p.epi == LVX_EPI_RESID_GATE_F32) {
+        if (p.gate != nullptr) gate = make_float4(p.gate[n], p.gate[n + 1], p.gate[n + 2], p.gate[n + 3]);
 #pragma unroll
         for (int c = 0; c < MB; ++c) {
-            if (A8) {
-                uint4 v[2] = {make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
-                if (in) {
-                    v[0] = reinterpret_cast<const uint4 *>(a_row[c] + (size_t)128 * t)[0];
-                    v[1] = reinterpret_cast<const uint4 *>(a_row[c] + (size_t)128 * t)[1];
-                }
-                a[c][0] = fp8x8_bf16(v[0].x, v[0].y), a[c][1] = fp8x8_bf16(v[0].z, v[0].w);
-                a[c][2] = fp8x8_bf16(v[1].x, v[1].y), a[c][3] = fp8x8_bf16(v[1].z, v[1].w);
+            const int64_t m = m0 + 16 * c;
+            if (m >= p.M) continue;
+            if (p.epi == LVX_EPI_RESID_GATE)
+                r16[c] = *reinterpret_cast<const uint2 *>((const bf16_t *)p.R + m * p.ldr + n);
+            else
+                r32[c] = *reinterpret_cast<const float4 *>((const float *)p.R + m * p.ldr + n);
+        }
+    }
+#pragma unroll
+    for (int c = 0; c < MB; ++c) {
+        const int64_t m = m0 + 16 * c;
+        if (m >= p.M) continue;
+        float v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = acc[c][i] * row_scale[c];
+        if (p.epi == LVX_EPI_GELU_TANH) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = gelu_tanh_f32(v[i]);
+        } else if (p.epi == LVX_EPI_RESID_GATE) {
+            v[0] = v[0] * gate.x + bf16_lo(r16[c].x), v[1] = v[1] * gate.y + bf16_hi(r16[c].x);
+            v[2] = v[2] * gate.z + bf16_lo(r16[c].y), v[3] = v[3] * gate.w + bf16_hi(r16[c].y);
+        } else if (p.epi == LVX_EPI_RESID_GATE_F32) {
+            v[0] = v[0] * gate.x + r32[c].x, v[1] = v[1] * gate.y + r32[c].y, v[2] = v[2] * gate.z + r32[c].z, v[3] = v[3] * gate.w + r32[c].w;
+        }
+        if (p.epi == LVX_EPI_RESID_GATE_F32 || p.epi == LVX_EPI_STORE_F32)
+            *reinterpret_cast<float4 *>((float *)p.C + m * p.ldc + n) = make_float4(v[0], v[1], v[2], v[3]);
+        else
+            *reinterpret_cast<uint2 *>((bf16_t *)p.C + m * p.ldc + n) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+    }
+}
+
+// this lane's rows' scales (1 for bf16 rows)
+template <int MODE, int MB>
+__device__ __forceinline__ void fp4_row_scales(const fp4_args_t &p, int m0, float (&s)[MB]) {
+#pragma unroll
+    for (int c = 0; c < MB; ++c) {
+        const int m = m0 + 16 * c;
+        s[c] = MODE == 0 ? 1.0f : p.row_scales[m < p.M ? m : p.M - 1];
+    }
+}
+
+// How the rows of A become operands: bf16 as they are; E4M3 widened to bf16 (exact, every product is); or E4M3 against E2M1 in one instruction.
+enum { A_BF16 = 0, A_WIDEN = 1, A_NATIVE = 2 };
+
+// Matrix products of a step of 128 channels: w[b] the codes of 16 columns, s[b] their scale as a byte (native) or as fp32 bits (widened codes), a[c] the operands of 16 rows.
+template <int MODE, int MB, int NB>
+__device__ __forceinline__ void fp4_multiply(f32x4_t (&acc)[NB][MB], const uint4 (&w)[NB], const uint32_t (&s)[NB], const uint4 (&a)[MB][MODE == A_BF16 ? 4 : 2]) {
+    if (MODE == A_NATIVE) {
+        i32x8_t av[MB];
+#pragma unroll
+        for (int c = 0; c < MB; ++c)
+            av[c] = {(int)a[c][0].x, (int)a[c][0].y, (int)a[c][0].z, (int)a[c][0].w, (int)a[c][1].x, (int)a[c][1].y, (int)a[c][1].z, (int)a[c][1].w};
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            const i32x8_t wv = {(int)w[b].x, (int)w[b].y, (int)w[b].z, (int)w[b].w, 0, 0, 0, 0};
+#pragma unroll
+            for (int c = 0; c < MB; ++c)  // formats: 4 = E2M1, 0 = E4M3; the rows' block scales are 2^0
+                acc[b][c] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wv, av[c], acc[b][c], 4, 0, 0, (int)s[b], 0, 127);
+        }
+    } else {
+        bf16x8_t x[MB][4];
+#pragma unroll
+        for (int c = 0; c < MB; ++c) {
+            if (MODE == A_WIDEN) {
+                x[c][0] = fp8x8_bf16(a[c][0].x, a[c][0].y), x[c][1] = fp8x8_bf16(a[c][0].z, a[c][0].w);
+                x[c][2] = fp8x8_bf16(a[c][1].x, a[c][1].y), x[c][3] = fp8x8_bf16(a[c][1].z, a[c][1].w);
             } else {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    uint4 v = make_uint4(0, 0, 0, 0);
-                    if (in) v = reinterpret_cast<const uint4 *>(a_row[c] + (size_t)256 * t)[j];
-                    a[c][j] = *reinterpret_cast<bf16x8_t *>(&v);
-                }
+                for (int j = 0; j < 4; ++j) x[c][j] = *reinterpret_cast<const bf16x8_t *>(&a[c][j % (MODE == A_BF16 ? 4 : 2)]);
             }
         }
 #pragma unroll
@@ -118,35 +114,311 @@ __global__ void __launch_bounds__(64 * KW) lvx_fp4_linear_kernel(fp4_args_t p) {
             const uint32_t words[4] = {w[b].x, w[b].y, w[b].z, w[b].w};
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const bf16x8_t wj = lvx_fp4x8_bf16(words[j], s[b]);
+                const bf16x8_t wj = lvx_fp4x8_bf16(words[j], __uint_as_float(s[b]));
 #pragma unroll
-                for (int c = 0; c < MB; ++c) acc[b][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wj, a[c][j], acc[b][c], 0, 0, 0);
+                for (int c = 0; c < MB; ++c) acc[b][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wj, x[c][j], acc[b][c], 0, 0, 0);
             }
         }
     }
+}
 
-    if (KW > 1) {
+__device__ __forceinline__ void swap32(uint32_t &a, uint32_t &b) {  // upper half of a <-> lower half of b
+    const auto r = __builtin_amdgcn_permlane32_swap(a, b, false, false);
+    a = r[0], b = r[1];
+}
+__device__ __forceinline__ void swap16(uint32_t &a, uint32_t &b) {  // odd rows of 16 lanes of a <-> even rows of b
+    const auto r = __builtin_amdgcn_permlane16_swap(a, b, false, false);
+    a = r[0], b = r[1];
+}
+
+constexpr int PANEL = 64;  // steps whose scales are held in LDS
+
+// ---- few rows: a wave per 16 NB columns and range of K -----------------------------------------------------------------
+// Bound by the weights' way from HBM.  A workgroup of blockDim.x / 64 waves owns 16 NB columns and 16 MB rows; the waves take units of U steps of 128 channels in turn.
+// Rows of A are loaded as runs of 64 bytes per row and instruction and exchanged between the lanes (piece 4 j + g of 16 bytes is loaded, 4 g + j is multiplied), scales
+// as U words per column: what counts here is the number of cache lines that the loads touch, not their bytes.
+template <int MODE, int MB, int NB, int U>
+__global__ void __launch_bounds__(512) lvx_fp4_few_kernel(fp4_args_t p) {
+    constexpr int AV = MODE == A_BF16 ? 4 : 2, STEP_A = MODE == A_BF16 ? 256 : 128;
+    extern __shared__ f32x4_t part[];  // [waves - 1][NB * MB][64]
+    const int lane = threadIdx.x & 63, kw = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    const int r = lane & 15, g = lane >> 4;
+    const int n0 = blockIdx.x * 16 * NB, m0 = blockIdx.y * 16 * MB;
+    const uint8_t *w_row[NB], *s_row[NB];
+    const char *a_row[MB];
+    // columns past the end repeat the last one: they are read, multiplied and not stored
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
-#pragma unroll
-            for (int c = 0; c < MB; ++c) part[wave][b * MB + c][lane] = acc[b][c];
-        __syncthreads();
+    for (int b = 0; b < NB; ++b) {
+        const int n = n0 + 16 * b + r < p.N ? n0 + 16 * b + r : p.N - 1;
+        w_row[b] = p.W + n * p.ldw + 16 * g;
+        s_row[b] = p.S + n * p.lds;
     }
-    // the blocks are shared out over the waves; the partial sums are added in the order of the waves
+#pragma unroll
+    for (int c = 0; c < MB; ++c) {
+        const int m = m0 + 16 * c + r < p.M ? m0 + 16 * c + r : p.M - 1;
+        a_row[c] = p.A + m * p.lda + 16 * g;
+    }
+    const bool row_in = MB > 1 || m0 + r < p.M;  // one block of rows: lanes of rows past the end load nothing
+    f32x4_t acc[NB][MB];
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
-        for (int c = 0; c < MB; ++c) {
-            if (KW > 1 && (b * MB + c) % KW != wave) continue;
-            f32x4_t v = acc[b][c];
-            if (KW > 1) {
-                v = part[0][b * MB + c][lane];
+        for (int c = 0; c < MB; ++c) acc[b][c] = {0, 0, 0, 0};
+
+    // the lanes' exchange: 4 x 4 pieces of a row over registers and lane groups are transposed; of eight pieces, a lane group gets 2 g and 2 g + 1
+    auto exchange = [&](uint4 (&v)[AV]) {
+        uint32_t *x[AV];
 #pragma unroll
-                for (int k = 1; k < KW; ++k) v += part[k][b * MB + c][lane];
+        for (int j = 0; j < AV; ++j) x[j] = reinterpret_cast<uint32_t *>(&v[j]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (MODE == A_BF16) {
+                swap32(x[0][e], x[2 % AV][e]), swap32(x[1][e], x[3 % AV][e]);
+                swap16(x[0][e], x[1][e]), swap16(x[2 % AV][e], x[3 % AV][e]);
+            } else {
+                swap32(x[0][e], x[1][e]);
+                swap16(x[0][e], x[1][e]);
             }
-            const int m = m0 + 16 * c + r, n = n0 + 16 * b + 4 * g;
-            if (m < p.M && n < p.N) fp4_store(p, m, n, v);
         }
+    };
+    const int whole = p.K / 128, units = whole / U, steps = (p.K + 127) / 128;
+    uint4 w[U][NB], a[U][MB][AV];
+    for (int u = kw; u < units; u += waves) {
+        uint32_t s[NB][U];
+#pragma unroll
+        for (int i = 0; i < U; ++i)
+#pragma unroll
+            for (int b = 0; b < NB; ++b) w[i][b] = *reinterpret_cast<const uint4 *>(w_row[b] + (size_t)64 * (u * U + i));
+#pragma unroll
+        for (int b = 0; b < NB; ++b) __builtin_memcpy(s[b], s_row[b] + (size_t)4 * U * u, 4 * U);
+#pragma unroll
+        for (int i = 0; i < U; ++i)
+#pragma unroll
+            for (int c = 0; c < MB; ++c)
+#pragma unroll
+                for (int j = 0; j < AV; ++j) {
+                    a[i][c][j] = make_uint4(0, 0, 0, 0);
+                    if (row_in) a[i][c][j] = *reinterpret_cast<const uint4 *>(a_row[c] + (size_t)STEP_A * (u * U + i) + 64 * j);
+                }
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            uint32_t sc[NB];
+#pragma unroll
+            for (int b = 0; b < NB; ++b) sc[b] = ((s[b][i] >> (8 * g)) & 255u) << 23;
+#pragma unroll
+            for (int c = 0; c < MB; ++c) exchange(a[i][c]);
+            fp4_multiply<MODE, MB, NB>(acc, w[i], sc, a[i]);
+        }
+    }
+    // the steps behind the whole units, the last of them with one to three groups of 32 channels: the other lanes multiply zeros
+    for (int t = units * U + kw; t < steps; t += waves) {
+        const int left = p.K - 128 * t;
+        uint32_t sc[NB];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            w[0][b] = make_uint4(0, 0, 0, 0), sc[b] = 127u << 23;
+            if (32 * g < left) {
+                w[0][b] = *reinterpret_cast<const uint4 *>(w_row[b] + (size_t)64 * t);
+                sc[b] = (uint32_t)s_row[b][(size_t)4 * t + g] << 23;
+            }
+        }
+#pragma unroll
+        for (int c = 0; c < MB; ++c) {
+#pragma unroll
+            for (int j = 0; j < AV; ++j) {
+                a[0][c][j] = make_uint4(0, 0, 0, 0);
+                if (row_in && (4 * j + g) * (MODE == A_BF16 ? 8 : 16) < left)
+                    a[0][c][j] = *reinterpret_cast<const uint4 *>(a_row[c] + (size_t)STEP_A * t + 64 * j);
+            }
+            exchange(a[0][c]);
+        }
+        fp4_multiply<MODE, MB, NB>(acc, w[0], sc, a[0]);
+    }
+
+    float row_scale[MB];
+    fp4_row_scales<MODE, MB>(p, m0 + r, row_scale);
+    if (kw > 0) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int c = 0; c < MB; ++c) part[((kw - 1) * NB * MB + b * MB + c) * 64 + lane] = acc[b][c];
+    }
+    __syncthreads();
+    if (kw > 0) return;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+#pragma unroll
+        for (int c = 0; c < MB; ++c)
+            for (int k = 1; k < waves; ++k) acc[b][c] += part[((k - 1) * NB * MB + b * MB + c) * 64 + lane];
+        fp4_store<MB>(p, m0 + r, n0 + 16 * b + 4 * g, acc[b], row_scale);
+    }
+}
+
+// ---- many rows: tiles of 16 MB rows and 128 columns ---------------------------------------------------------------------
+// Bound by the matrix cores.  Eight waves: two beside each other over the columns (64 each, whose weights go straight into registers), four groups over K, every
+// fourth step each, with the rows of A in LDS, a step ahead.  A row of a stage is 128 (8 bits) or 256 bytes; its 16-byte chunk c lies at c ^ (row % 8 or 16), so that
+// the sixteen rows of an operand fall into different banks.
+template <int MODE, int MB>
+__global__ void __launch_bounds__(512) lvx_fp4_tile_kernel(fp4_args_t p) {
+    constexpr int NB = 4, KG = 4, AV = MODE == A_BF16 ? 4 : 2, ROW = MODE == A_BF16 ? 256 : 128, CH = ROW / 16;
+    constexpr int STAGE = MB * 16 * ROW;
+    extern __shared__ char lds[];  // [KG][2][STAGE], then the partial sums
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int nw = wave & 1, kg = wave >> 1;
+    const int r = lane & 15, g = lane >> 4;
+    const int n0 = blockIdx.x * 128 + nw * 64, m0 = blockIdx.y * 16 * MB;
+    __shared__ uint32_t scales[128 * (PANEL + 1)];
+    const uint8_t *w_row[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+        const int n = n0 + 16 * b + r < p.N ? n0 + 16 * b + r : p.N - 1;
+        w_row[b] = p.W + n * p.ldw + 16 * g;
+    }
+    // this wave's half of the group's stage: row and chunk of each lane's 16 bytes per instruction
+    constexpr int DMAS = STAGE / 1024 / 2, ROWS_PER = 1024 / ROW;
+    uint32_t a_off[DMAS];
+#pragma unroll
+    for (int i = 0; i < DMAS; ++i) {
+        const int row = (nw * DMAS + i) * ROWS_PER + lane / CH;
+        const int m = m0 + row < p.M ? row : p.M - 1 - m0;
+        a_off[i] = (uint32_t)(m * p.lda);
+    }
+    const char *a_base = p.A + (int64_t)m0 * p.lda;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds + kg * 2 * STAGE + nw * (STAGE / 2);
+    f32x4_t acc[NB][MB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int c = 0; c < MB; ++c) acc[b][c] = {0, 0, 0, 0};
+
+    const int steps = (p.K + 127) / 128;
+    auto stage = [&](int t, int buf) {
+        const int chunks = (p.K - 128 * t) * (ROW / 128) / 16;  // of the last step, those behind K are not read: the first is, in their place, and not used
+#pragma unroll
+        for (int i = 0; i < DMAS; ++i) {
+            uint32_t c = ((uint32_t)(lane % CH)) ^ (uint32_t)(((nw * DMAS + i) * ROWS_PER + lane / CH) % CH);
+            c = (int)c < chunks ? c : 0;
+            lvx_dma16(a_base, a_off[i] + (uint32_t)t * ROW + 16 * c, lds0 + buf * STAGE + i * 1024);
+        }
+    };
+    auto fetch = [&](int t, uint4 (&w)[NB]) {
+        const bool in = 128 * t + 32 * g < p.K;
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            w[b] = make_uint4(0, 0, 0, 0);
+            if (in) w[b] = *reinterpret_cast<const uint4 *>(w_row[b] + (size_t)64 * t);
+        }
+    };
+    // A group takes every fourth pair of steps: a pair is a whole line of a weight row.
+    const int pairs = (steps + 1) / 2, rounds = (pairs + KG - 1) / KG;
+    uint4 w[2][2][NB];
+    auto fetch_pair = [&](int q, uint4 (&d)[2][NB]) {
+        if (2 * q < steps) fetch(2 * q, d[0]);
+        if (2 * q + 1 < steps) fetch(2 * q + 1, d[1]);
+    };
+    if (2 * kg < steps) stage(2 * kg, 0), fetch_pair(kg, w[0]);
+    auto step = [&](int t, int next, int buf, uint4 (&wi)[NB]) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        if (next < steps) stage(next, buf ^ 1);
+        if (t < steps) {
+            const char *src = lds + (kg * 2 + buf) * STAGE + r * ROW;
+            const uint8_t *mine = reinterpret_cast<const uint8_t *>(scales + (nw * 64 + r) * (PANEL + 1) + t % PANEL) + g;
+            uint4 a[MB][AV];
+            const int left = p.K - 128 * t;
+#pragma unroll
+            for (int c = 0; c < MB; ++c)
+#pragma unroll
+                for (int j = 0; j < AV; ++j) {
+                    const int chunk = MODE == A_BF16 ? 4 * g + j : MODE == A_WIDEN ? 2 * g + j : g + 4 * j;
+                    a[c][j] = *reinterpret_cast<const uint4 *>(src + c * 16 * ROW + 16 * (chunk ^ (r % CH)));
+                }
+            uint32_t sc[NB];
+#pragma unroll
+            for (int b = 0; b < NB; ++b) sc[b] = (uint32_t)mine[16 * b * (PANEL + 1) * 4] << (MODE == A_NATIVE ? 0 : 23);
+            if (left < 128) {
+#pragma unroll
+                for (int c = 0; c < MB; ++c)
+#pragma unroll
+                    for (int j = 0; j < AV; ++j)
+                        if ((MODE == A_NATIVE ? 16 * g + 64 * j : 32 * g) >= left) a[c][j] = make_uint4(0, 0, 0, 0);
+#pragma unroll
+                for (int b = 0; b < NB; ++b) sc[b] = 32 * g < left ? sc[b] : 127u << (MODE == A_NATIVE ? 0 : 23);
+            }
+            fp4_multiply<MODE, MB, NB>(acc, wi, sc, a);
+        }
+    };
+    auto round = [&](int i, uint4 (&wi)[2][NB], uint4 (&wn)[2][NB]) {
+        const int q = kg + KG * i;
+        if (i % (PANEL / 2 / KG) == 0) {
+            // the next 64 steps' scales, 16 bytes = 4 steps of a column a piece
+            if (i > 0) __syncthreads();
+            const int b0 = 2 * KG * 4 * i, row_bytes = p.K / 32;
+            uint4 v[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int piece = threadIdx.x + 512 * j, row = piece >> 4, at = b0 + 16 * (piece & 15);
+                const int n = blockIdx.x * 128 + row < p.N ? blockIdx.x * 128 + row : p.N - 1;
+                const uint8_t *src = p.S + n * p.lds + at;
+                v[j] = make_uint4(0, 0, 0, 0);
+                if (at + 16 <= row_bytes) {
+                    __builtin_memcpy(&v[j], src, 16);
+                } else if (at < row_bytes) {
+                    uint32_t e[4] = {0, 0, 0, 0};
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        if (at + 4 * k + 4 <= row_bytes) {
+                            __builtin_memcpy(&e[k], src + 4 * k, 4);
+                        } else {
+#pragma unroll
+                            for (int x = 0; x < 3; ++x)
+                                if (at + 4 * k + x < row_bytes) e[k] |= (uint32_t)src[4 * k + x] << (8 * x);
+                        }
+                    }
+                    v[j] = make_uint4(e[0], e[1], e[2], e[3]);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int piece = threadIdx.x + 512 * j;
+                uint32_t *dst = scales + (piece >> 4) * (PANEL + 1) + 4 * (piece & 15);
+                dst[0] = v[j].x, dst[1] = v[j].y, dst[2] = v[j].z, dst[3] = v[j].w;
+            }
+        }
+        step(2 * q, 2 * q + 1, 0, wi[0]);
+        if (2 * (q + KG) < steps) fetch_pair(q + KG, wn);
+        step(2 * q + 1, 2 * (q + KG), 1, wi[1]);
+    };
+    for (int i = 0; i < rounds; i += 2) {
+        round(i, w[0], w[1]);
+        if (i + 1 < rounds) round(i + 1, w[1], w[0]);
+    }
+    __syncthreads();
+
+    float row_scale[MB];
+    fp4_row_scales<MODE, MB>(p, m0 + r, row_scale);
+    // the groups' sums: 2 and 3 to 0 and 1, then 1 to 0
+    f32x4_t *part = reinterpret_cast<f32x4_t *>(lds);
+#pragma unroll
+    for (int half = 2; half >= 1; half >>= 1) {
+        if (kg >= half && kg < 2 * half) {
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int c = 0; c < MB; ++c) part[(((kg - half) * 2 + nw) * NB * MB + b * MB + c) * 64 + lane] = acc[b][c];
+        }
+        __syncthreads();
+        if (kg < half) {
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int c = 0; c < MB; ++c) acc[b][c] += part[((kg * 2 + nw) * NB * MB + b * MB + c) * 64 + lane];
+        }
+        __syncthreads();
+    }
+    if (kg > 0) return;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) fp4_store<MB>(p, m0 + r, n0 + 16 * b + 4 * g, acc[b], row_scale);
 }
 
 // 32 channels of a row per thread
@@ -172,13 +444,71 @@ __global__ void __launch_bounds__(256) lvx_fp4_quant_kernel(const bf16_t *x, int
     }
 }
 
-template <int MB, int NB, int KW>
-void launch(const fp4_args_t &p, hipStream_t stream) {
+template <int MODE, int MB, int NB, int U>
+void launch_few(const fp4_args_t &p, int most_waves, hipStream_t stream) {
+    // as many waves as share the units of U steps evenly
+    const int units = (p.K + 128 * U - 1) / (128 * U), rounds = (units + most_waves - 1) / most_waves, waves = (units + rounds - 1) / rounds;
     const dim3 grid((p.N + 16 * NB - 1) / (16 * NB), (p.M + 16 * MB - 1) / (16 * MB));
-    if (p.row_scales != nullptr)
-        hipLaunchKernelGGL((lvx_fp4_linear_kernel<MB, NB, KW, true>), grid, dim3(64 * KW), 0, stream, p);
+    hipLaunchKernelGGL((lvx_fp4_few_kernel<MODE, MB, NB, U>), grid, dim3(64 * waves), (waves - 1) * NB * MB * 1024, stream, p);
+}
+
+template <int MODE, int MB>
+void launch_tile(const fp4_args_t &p, hipStream_t stream) {
+    const dim3 grid((p.N + 127) / 128, (p.M + 16 * MB - 1) / (16 * MB));
+    const int stages = 4 * 2 * MB * 16 * (MODE == A_BF16 ? 256 : 128), sums = 2 * 2 * 4 * MB * 1024;
+    hipLaunchKernelGGL((lvx_fp4_tile_kernel<MODE, MB>), grid, dim3(512), stages > sums ? stages : sums, stream, p);
+}
+
+// Few rows.  More columns to a workgroup share the loads of A; that pays where enough workgroups are left (5120 columns, 5120 channels, 4 rows: 8.2 us with two blocks of
+// columns, 8.9 with one; 13824 columns, 16 rows in bf16: 14.3 with four, 17.5 with two; 1280 columns: one is fastest).
+template <int MODE>
+void linear_few(const fp4_args_t &p, hipStream_t stream) {
+    const int blocks = (p.M + 15) / 16, tiles = (blocks + 3) / 4, mb = (blocks + tiles - 1) / tiles;
+    const bool two = p.N >= 4096;
+    if (mb == 1)
+        p.N >= 12800 ? launch_few<MODE, 1, 4, 2>(p, 8, stream) : two ? launch_few<MODE, 1, 2, 2>(p, 8, stream) : launch_few<MODE, 1, 1, 2>(p, 8, stream);
+    else if (mb == 2)
+        two ? launch_few<MODE, 2, 2, 2>(p, 5, stream) : launch_few<MODE, 2, 1, 2>(p, 5, stream);
+    else if (mb == 3)
+        two ? launch_few<MODE, 3, 2, 2>(p, 5, stream) : launch_few<MODE, 3, 1, 2>(p, 5, stream);
     else
-        hipLaunchKernelGGL((lvx_fp4_linear_kernel<MB, NB, KW, false>), grid, dim3(64 * KW), 0, stream, p);
+        two ? launch_few<MODE, 4, 2, MODE == A_BF16 ? 1 : 2>(p, 4, stream) : launch_few<MODE, 4, 1, MODE == A_BF16 ? 1 : 2>(p, 4, stream);
+}
+
+// Rows of a tile, in blocks of 16: the fewest rounds of the chip, weighed with what a round costs.  A step takes about as long as 8 blocks of 8-bit rows (4 of bf16) even
+// without any (its loads' way); measured at 5120 channels, one round: 22, 26 and 31 us with 2, 4 and 6 blocks of 8-bit rows.
+int tile_blocks(const fp4_args_t &p, const int *choices, int n, int cost_of_block) {
+    int best = 0;
+    int64_t least = INT64_MAX;
+    for (int i = 0; i < n; ++i) {
+        const int64_t groups = (int64_t)((p.N + 127) / 128) * ((p.M + 16 * choices[i] - 1) / (16 * choices[i]));
+        const int64_t cost = (groups + LVX_NUM_CU - 1) / LVX_NUM_CU * (8 + cost_of_block * choices[i]);
+        if (cost < least) least = cost, best = choices[i];
+    }
+    return best;
+}
+
+void linear_launch(const fp4_args_t &p, bool a8, hipStream_t stream) {
+    // Tiles from the product of rows (in blocks) and columns on where they fill the chip and are faster (bf16: 96 x 5120 x 1280 10.7 us against 12.8, 96 x 1280 x 1280 10.4
+    // against 8.3; 8-bit rows: 96 x 13824 x 5120 29 against 47, 48 x 13824 x 1280 13.7 against 9.5), and rows within reach of the tiles' 32-bit offsets.
+    const int64_t area = (int64_t)((p.M + 15) / 16) * p.N;
+    const bool tiles = p.M > 32 && area >= (a8 ? 50000 : 24000) && p.lda < (1 << 24);
+    if (!tiles) {
+        a8 ? linear_few<A_WIDEN>(p, stream) : linear_few<A_BF16>(p, stream);
+    } else if (!a8) {
+        static const int choices[] = {3, 2, 1};
+        const int mb = tile_blocks(p, choices, 3, 2);
+        mb == 3 ? launch_tile<A_BF16, 3>(p, stream) : mb == 2 ? launch_tile<A_BF16, 2>(p, stream) : launch_tile<A_BF16, 1>(p, stream);
+    } else if (p.epi == LVX_EPI_RESID_GATE_F32 || p.epi == LVX_EPI_STORE_F32) {
+        // The mixed instruction aligns the 128 products of a step before it adds them and drops what lies about 2^-17 below the largest: nothing beside a bf16 output's rounding,
+        // but more than fp32 sums lose.  Outputs in fp32 get the rows widened to bf16.
+        static const int choices[] = {4, 2};
+        tile_blocks(p, choices, 2, 2) == 4 ? launch_tile<A_WIDEN, 4>(p, stream) : launch_tile<A_WIDEN, 2>(p, stream);
+    } else {
+        static const int choices[] = {6, 4, 2};
+        const int mb = tile_blocks(p, choices, 3, 1);
+        mb == 6 ? launch_tile<A_NATIVE, 6>(p, stream) : mb == 4 ? launch_tile<A_NATIVE, 4>(p, stream) : launch_tile<A_NATIVE, 2>(p, stream);
+    }
 }
 
 lvx_status_t linear(const void *a, int64_t lda, const float *row_scales, bool a8, const void *w, int64_t ldw, const void *s, int64_t lds, void *c,
@@ -210,12 +540,7 @@ lvx_status_t linear(const void *a, int64_t lda, const float *row_scales, bool a8
     p.R = resid, p.ldr = ldr;
     p.gate = gate;
     p.M = M, p.N = N, p.K = K, p.epi = (int)epi;
-    if (M <= 16)
-        launch<1, 1, 8>(p, stream);
-    else if (M <= 32)
-        launch<2, 1, 8>(p, stream);
-    else
-        launch<4, 4, 1>(p, stream);
+    linear_launch(p, a8, stream);
     LVX_CHECK_HIP(hipGetLastError());
     return LVX_OK;
 }
