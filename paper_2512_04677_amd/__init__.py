@@ -154,12 +154,13 @@ def _check(status):
 
 
 def _ptr(t):
-    return None if t is None else C.c_void_p(t.data_ptr())
+    return None if t is None else t.data_ptr()
 
 
 def _stream():
+    """The current HIP stream of the current device, as an address (looked up without building a torch.cuda.Stream: 2 us of a small call's 8)."""
     import torch
-    return C.c_void_p(torch.cuda.current_stream().cuda_stream)
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
 def version():
@@ -339,22 +340,25 @@ def lvx_layernorm_modulate(x, shift, scale, eps, u):
 
 def _norm_args(x, resid, gain, eps, sum_out):
     import torch
-    ref = x if x is not None else resid
-    return (_ptr(x), x.stride(0) if x is not None else 0, _ptr(resid), resid.stride(0) if resid is not None else 0,
-            1 if resid is not None and resid.dtype == torch.float32 else 0, _ptr(gain), eps, ref.shape[0], ref.shape[1], _ptr(sum_out),
-            sum_out.stride(0) if sum_out is not None else 0)
+    n, d = (resid if x is None else x).shape
+    return (_ptr(x), 0 if x is None else x.stride(0), _ptr(resid), 0 if resid is None else resid.stride(0),
+            0 if resid is None or resid.dtype != torch.float32 else 1, _ptr(gain), eps, n, d, _ptr(sum_out), 0 if sum_out is None else sum_out.stride(0))
 
 
 def lvx_rmsnorm_residual(x, resid, gain, eps, y, sum_out=None):
-    """y = RMSNorm(x + resid) * gain in bf16; sum_out (the residual's dtype) receives x + resid.  x or resid may be None."""
+    """y = RMSNorm(x + resid) * gain in bf16; sum_out (the residual's dtype) receives x + resid.  x or resid may be None.  No rows: nothing is done."""
     _check_like(resid, sum_out)
-    _check(load().lvx_rmsnorm_residual(*_norm_args(x, resid, gain, eps, sum_out), _ptr(y), y.stride(0), _stream()))
+    a = _norm_args(x, resid, gain, eps, sum_out)
+    if a[7]:
+        _check(load().lvx_rmsnorm_residual(*a, y.data_ptr(), y.stride(0), _stream()))
 
 
 def lvx_rmsnorm_residual_fp8(x, resid, gain, eps, q, row_scales, sum_out=None):
     """The same with y as E4M3 codes (uint8 [n][>= d]) and one fp32 scale a row."""
     _check_like(resid, sum_out)
-    _check(load().lvx_rmsnorm_residual_fp8(*_norm_args(x, resid, gain, eps, sum_out), _ptr(q), q.stride(0), _ptr(row_scales), _stream()))
+    a = _norm_args(x, resid, gain, eps, sum_out)
+    if a[7]:
+        _check(load().lvx_rmsnorm_residual_fp8(*a, q.data_ptr(), q.stride(0), row_scales.data_ptr(), _stream()))
 
 
 def _check_like(resid, sum_out):
@@ -375,16 +379,20 @@ def lvx_fp4_quantize(x, q=None, scales=None):
 
 
 def lvx_linear_fp4(a, wq, w_scales, c, epi=EPI_STORE, resid=None, gate=None):
-    """c = epilogue(a [M][K] bf16 times the E2M1 weights wq [N][K / 2] with scales [N][K / 32], transposed)."""
-    _check(load().lvx_linear_fp4(_ptr(a), a.stride(0), _ptr(wq), wq.stride(0), _ptr(w_scales), w_scales.stride(0), _ptr(c), c.stride(0), a.shape[0],
-                                 wq.shape[0], a.shape[1], epi, _ptr(resid), resid.stride(0) if resid is not None else 0, _ptr(gate), _stream()))
+    """c = epilogue(a [M][K] bf16 times the E2M1 weights wq [N][K / 2] with scales [N][K / 32], transposed).  No rows: nothing is done."""
+    M, K = a.shape
+    if M:
+        _check(load().lvx_linear_fp4(a.data_ptr(), a.stride(0), wq.data_ptr(), wq.stride(0), w_scales.data_ptr(), w_scales.stride(0), c.data_ptr(),
+                                     c.stride(0), M, wq.shape[0], K, epi, _ptr(resid), 0 if resid is None else resid.stride(0), _ptr(gate), _stream()))
 
 
 def lvx_linear_fp8_fp4(aq, row_scales, wq, w_scales, c, epi=EPI_STORE, resid=None, gate=None):
     """The same for E4M3 rows (uint8 [M][K]) with one fp32 scale each."""
-    _check(load().lvx_linear_fp8_fp4(_ptr(aq), aq.stride(0), _ptr(row_scales), _ptr(wq), wq.stride(0), _ptr(w_scales), w_scales.stride(0), _ptr(c),
-                                     c.stride(0), aq.shape[0], wq.shape[0], aq.shape[1], epi, _ptr(resid), resid.stride(0) if resid is not None else 0,
-                                     _ptr(gate), _stream()))
+    M, K = aq.shape
+    if M:
+        _check(load().lvx_linear_fp8_fp4(aq.data_ptr(), aq.stride(0), row_scales.data_ptr(), wq.data_ptr(), wq.stride(0), w_scales.data_ptr(),
+                                         w_scales.stride(0), c.data_ptr(), c.stride(0), M, wq.shape[0], K, epi, _ptr(resid),
+                                         0 if resid is None else resid.stride(0), _ptr(gate), _stream()))
 
 
 def kv4_desc(n_layers, n_seqs, n_kv_heads, head_dim, max_keys):
@@ -420,10 +428,12 @@ class KV4Cache:
 
 def lvx_kv4_append(cache, layer, k, v, key_counts, starts=None, max_tokens=1, n_tokens=None):
     """k, v: bf16 [n_tokens][kv heads * head_dim] of one row stride; key_counts, starts: device int32."""
-    if k.stride(0) != v.stride(0):
+    ld = k.stride(0)
+    if ld != v.stride(0):
         raise LvxError(2, "k and v must share their row stride")
-    _check(load().lvx_kv4_append(cache.handle, layer, _ptr(k), _ptr(v), k.stride(0), _ptr(starts), k.shape[0] if n_tokens is None else n_tokens, max_tokens,
-                                 _ptr(key_counts), _stream()))
+    n = k.shape[0] if n_tokens is None else n_tokens
+    if n:
+        _check(load().lvx_kv4_append(cache.handle, layer, k.data_ptr(), v.data_ptr(), ld, _ptr(starts), n, max_tokens, key_counts.data_ptr(), _stream()))
 
 
 def lvx_kv4_gather(cache, layer, key_counts, k_out, v_out, first_key=0):
@@ -442,10 +452,11 @@ def lvx_kv4_attention_workspace_bytes(cache, n_heads, max_tokens):
 
 
 def lvx_kv4_attention(cache, layer, q, n_heads, scale, key_counts, out, workspace, starts=None, max_tokens=1, causal=True, n_tokens=None):
-    """q, out: bf16 [n_tokens][heads * head_dim]; workspace: lvx_kv4_attention_workspace_bytes(cache, n_heads, max_tokens) bytes."""
-    _check(load().lvx_kv4_attention(cache.handle, layer, _ptr(q), q.stride(0), n_heads, _ptr(starts), q.shape[0] if n_tokens is None else n_tokens, max_tokens,
-                                    _ptr(key_counts), 1 if causal else 0, scale, _ptr(out), out.stride(0), _ptr(workspace),
-                                    workspace.numel() * workspace.element_size(), _stream()))
+    """q, out: bf16 [n_tokens][heads * head_dim] (no tokens: nothing is done); workspace: lvx_kv4_attention_workspace_bytes(cache, n_heads, max_tokens) bytes."""
+    n = q.shape[0] if n_tokens is None else n_tokens
+    if n:
+        _check(load().lvx_kv4_attention(cache.handle, layer, q.data_ptr(), q.stride(0), n_heads, _ptr(starts), n, max_tokens, key_counts.data_ptr(),
+                                        1 if causal else 0, scale, out.data_ptr(), out.stride(0), workspace.data_ptr(), workspace.nbytes, _stream()))
 
 
 class StageHandle:
