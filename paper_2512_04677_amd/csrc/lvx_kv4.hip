@@ -213,7 +213,7 @@ struct attn_args_t {
 // Rows of a workgroup: (token, head of the group) pairs of one sequence and kv head, row = token * group + head, 16 RB per wave, WR waves side by side;
 // WK waves share the keys, every WK-th tile each.
 template <int D, int RB, int WR, int WK>
-__global__ void __launch_bounds__(64 * WR * WK) lvx_kv4_attention_kernel(attn_args_t p) {
+__global__ void __launch_bounds__(64 * WR * WK, 2) lvx_kv4_attention_kernel(attn_args_t p) {
     typedef tile_t<D> T;
     constexpr int CB = D / 16, KS = D / 32;  // channel blocks, steps of 32 channels
     constexpr int SLOT = RB * (CB * 4 + 2);  // floats a lane leaves for the joining
@@ -265,26 +265,33 @@ __global__ void __launch_bounds__(64 * WR * WK) lvx_kv4_attention_kernel(attn_ar
     }
 
     const uint8_t *rec0 = p.base + s * p.seq_stride + head * p.head_stride;
+    uint4 kq[D / 32];
+    uint32_t ks = 0;
+    auto load_keys = [&](int t) {
+        const uint8_t *rec = rec0 + (int64_t)t * T::BYTES;
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) kq[i] = *reinterpret_cast<const uint4 *>(rec + i * 1024 + lane * 16);
+        ks = *reinterpret_cast<const uint32_t *>(rec + T::KS + ((D == 128 ? g : g >> 1) * 16 + r) * 4);
+    };
+    if (t0 + wk < t1) load_keys(t0 + wk);
     for (int t = t0 + wk; t < t1; t += WK) {
         const uint8_t *rec = rec0 + (int64_t)t * T::BYTES;
+        uint4 vq[CB / 2], vsw[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) vsw[h] = *reinterpret_cast<const uint4 *>(rec + T::VS + 64 * h + 16 * g);
+#pragma unroll
+        for (int c2 = 0; c2 < CB / 2; ++c2) vq[c2] = *reinterpret_cast<const uint4 *>(rec + T::V + c2 * 1024 + lane * 16);
         // scores, transposed: a lane has four keys of each block for its query
         f32x4_t x[RB][4];
 #pragma unroll
         for (int b = 0; b < RB; ++b)
 #pragma unroll
             for (int kb = 0; kb < 4; ++kb) x[b][kb] = {0, 0, 0, 0};
-        const uint32_t ks = *reinterpret_cast<const uint32_t *>(rec + T::KS + ((D == 128 ? g : g >> 1) * 16 + r) * 4);
 #pragma unroll
         for (int kb = 0; kb < 4; ++kb) {
             const float scale = lvx_e8m0_f32((ks >> (8 * kb)) & 255u);
-            uint32_t w[4];
-            if (D == 128) {
-                const uint4 v = *reinterpret_cast<const uint4 *>(rec + kb * 1024 + lane * 16);
-                w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
-            } else {
-                const uint2 v = *reinterpret_cast<const uint2 *>(rec + (kb >> 1) * 1024 + lane * 16 + (kb & 1) * 8);
-                w[0] = v.x, w[1] = v.y;
-            }
+            const uint4 v = kq[D == 128 ? kb : kb >> 1];
+            const uint32_t w[4] = {D == 128 || (kb & 1) == 0 ? v.x : v.z, D == 128 || (kb & 1) == 0 ? v.y : v.w, v.z, v.w};
 #pragma unroll
             for (int j = 0; j < KS; ++j) {
                 const bf16x8_t kf = lvx_fp4x8_bf16(w[j], scale);
@@ -292,59 +299,88 @@ __global__ void __launch_bounds__(64 * WR * WK) lvx_kv4_attention_kernel(attn_ar
                 for (int b = 0; b < RB; ++b) x[b][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, q[b][j], x[b][kb], 0, 0, 0);
             }
         }
+        if (t + WK < t1) load_keys(t + WK);
         // softmax; lane's keys: 32 (kb / 2) + 8 g + 4 (kb % 2) + i
-        float vs[16];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const uint4 v = *reinterpret_cast<const uint4 *>(rec + T::VS + 64 * h + 16 * g);
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) vs[8 * h + 2 * e] = bf16_lo(w[e]), vs[8 * h + 2 * e + 1] = bf16_hi(w[e]);
-        }
+        const bool masked = TILE * (t + 1) > least;
         bf16x8_t pf[RB][2];
 #pragma unroll
         for (int b = 0; b < RB; ++b) {
             float y[16];
-            float m = -INFINITY;
-#pragma unroll
-            for (int kb = 0; kb < 4; ++kb)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) y[4 * kb + i] = x[b][kb][i] * p.scale_log2;
-            if (TILE * (t + 1) > least) {
+            float base = ref[b] == -INFINITY ? 0.f : ref[b], l = 0;
+            auto exponents = [&]() {
+                l = 0;
 #pragma unroll
                 for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (TILE * t + 32 * (kb >> 1) + 8 * g + 4 * (kb & 1) + i >= seen[b]) y[4 * kb + i] = -INFINITY;
+                    for (int i = 0; i < 4; ++i) y[4 * kb + i] = x[b][kb][i] * p.scale_log2 - base;
+                if (masked) {
+#pragma unroll
+                    for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (TILE * t + 32 * (kb >> 1) + 8 * g + 4 * (kb & 1) + i >= seen[b]) y[4 * kb + i] = -INFINITY;
+                }
+            };
+            auto powers = [&]() {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    y[i] = __builtin_amdgcn_exp2f(y[i]);
+                    l += y[i];
+                }
+            };
+            // The reference that is subtracted only has to keep the powers inside fp32.  With the running maximum the largest probability is 1 and its rounding exact, which
+            // peaked rows notice (errors of 1.7e-3 against 2.1e-3 with a reference that lags by up to 2^20): where the cache's bytes bound the kernel, that is what it is.
+            // Where the vector unit does (one wave per tile of keys), it is the first tile's maximum, and a tile whose powers reach 2^4 of it moves it (1.9e-3).
+            // A row without a reference sees none of the tiles so far, nor any later one (a row sees a prefix of the keys).
+            constexpr bool RUNNING = WK > 1;
+            bool move = t == t0 + wk;
+            float m = -INFINITY;
+            auto maximum = [&]() {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) m = fmaxf(m, y[i]);
+                m = fmaxf(m, __shfl_xor(m, 16));
+                m = fmaxf(m, __shfl_xor(m, 32));
+            };
+            exponents();
+            if (RUNNING) {
+                maximum();
+                move = move || __any(m > 0.f);
+            } else if (!move) {
+                powers();
+                move = __any(!(l < 0x1p4f));
+                if (move) exponents();
+            }
+            if (move) {
+                if (!RUNNING) maximum();
+                const float next = fmaxf(ref[b], m + base);
+                base = next == -INFINITY ? 0.f : next;
+                const float shrink = __builtin_amdgcn_exp2f(ref[b] - base);
+                ref[b] = next;
+                exponents();
+                sum[b] *= shrink;
+#pragma unroll
+                for (int c = 0; c < CB; ++c)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[b][c][i] *= shrink;
+            }
+            if (RUNNING || move) powers();
+            sum[b] += l;
+            // the probability times the value's scale, rounded to bf16 once
+            const uint32_t w[8] = {vsw[0].x, vsw[0].y, vsw[0].z, vsw[0].w, vsw[1].x, vsw[1].y, vsw[1].z, vsw[1].w};
+            float z[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) z[i] = y[i] * ((i & 1) ? bf16_hi(w[i >> 1]) : bf16_lo(w[i >> 1]));
+            if (masked) {  // a hidden key's scale may be anything
+#pragma unroll
+                for (int i = 0; i < 16; ++i) z[i] = y[i] == 0.f ? 0.f : z[i];
             }
 #pragma unroll
-            for (int i = 0; i < 16; ++i) m = fmaxf(m, y[i]);
-            m = fmaxf(m, __shfl_xor(m, 16));
-            m = fmaxf(m, __shfl_xor(m, 32));
-            const float next = fmaxf(ref[b], m);
-            const float base = next == -INFINITY ? 0.f : next;
-            const float shrink = __builtin_amdgcn_exp2f(ref[b] - base);
-            ref[b] = next;
-            float l = 0;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                y[i] = __builtin_amdgcn_exp2f(y[i] - base);
-                l += y[i];
-            }
-            sum[b] = sum[b] * shrink + l;
-#pragma unroll
-            for (int c = 0; c < CB; ++c)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) o[b][c][i] *= shrink;
-            // the probability times the value's scale, rounded to bf16 once; a hidden key's scale may be anything
-#pragma unroll
-            for (int i = 0; i < 16; ++i) pf[b][i >> 3][i & 7] = (__bf16)(y[i] == 0.f ? 0.f : y[i] * vs[i]);
+            for (int i = 0; i < 16; ++i) pf[b][i >> 3][i & 7] = (__bf16)z[i];
         }
         // outputs, transposed: a lane has four channels of each block for its query
 #pragma unroll
         for (int c2 = 0; c2 < CB / 2; ++c2) {
-            const uint4 v = *reinterpret_cast<const uint4 *>(rec + T::V + c2 * 1024 + lane * 16);
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+            const uint32_t w[4] = {vq[c2].x, vq[c2].y, vq[c2].z, vq[c2].w};
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const bf16x8_t vf = lvx_fp4x8_bf16(w[e], 1.0f);
@@ -566,17 +602,17 @@ namespace {
 
 constexpr int MAX_SPLITS = 64;
 
-// Rows per workgroup and ranges of keys of a call, by sizes that the host knows.  With 16 rows at most per sequence and kv head a workgroup takes one block
-// of 16 rows and its waves share the keys; with more, the waves stand side by side.  The keys are split into ranges while the workgroups leave compute
-// units idle and a range keeps at least 512 keys of a full cache.
+// Rows per workgroup and ranges of keys of a call, by sizes that the host knows.  A sequence's rows of a kv head (tokens x heads of the group) up to 16 are one block, with four
+// waves sharing the keys; two blocks a wave with four, two or one wave on the same keys up to 32, up to 64 and beyond.  The keys are split into ranges while the workgroups
+// leave compute units idle and a range keeps at least 512 keys of a full cache.
 struct attn_plan_t {
-    int few, row_tiles, splits;
+    int rows, row_tiles, splits;  // rows of a workgroup: 16, 32, 64 or 128
 };
 attn_plan_t attn_plan(const lvx_kv4_desc_t &d, int n_heads, int max_tokens) {
     attn_plan_t pl;
     const int64_t rows = (int64_t)max_tokens * (n_heads / d.n_kv_heads);
-    pl.few = rows <= 32;
-    pl.row_tiles = (int)((rows + (pl.few ? 15 : 127)) / (pl.few ? 16 : 128));
+    pl.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
+    pl.row_tiles = (int)((rows + pl.rows - 1) / pl.rows);
     const int64_t groups = (int64_t)pl.row_tiles * d.n_kv_heads * d.n_seqs;
     int64_t splits = groups > 0 ? 1024 / groups : 1;
     const int64_t most = d.max_keys / 512;
@@ -584,6 +620,18 @@ attn_plan_t attn_plan(const lvx_kv4_desc_t &d, int n_heads, int max_tokens) {
     splits = splits < MAX_SPLITS ? splits : MAX_SPLITS;
     pl.splits = (int)(splits > 1 ? splits : 1);
     return pl;
+}
+
+template <int D>
+void attn_launch(const attn_plan_t &pl, const attn_args_t &p, dim3 grid, hipStream_t stream) {
+    if (pl.rows == 16)
+        hipLaunchKernelGGL((lvx_kv4_attention_kernel<D, 1, 1, 4>), grid, dim3(256), 0, stream, p);
+    else if (pl.rows == 32)
+        hipLaunchKernelGGL((lvx_kv4_attention_kernel<D, 2, 1, 4>), grid, dim3(256), 0, stream, p);
+    else if (pl.rows == 64)
+        hipLaunchKernelGGL((lvx_kv4_attention_kernel<D, 2, 2, 2>), grid, dim3(256), 0, stream, p);
+    else
+        hipLaunchKernelGGL((lvx_kv4_attention_kernel<D, 2, 4, 1>), grid, dim3(256), 0, stream, p);
 }
 
 uint64_t attn_scratch(const lvx_kv4_desc_t &d, int n_heads, int max_tokens) {
@@ -640,17 +688,7 @@ extern "C" lvx_status_t lvx_kv4_attention(const lvx_kv4_t *cache, int32_t layer,
     p.part_o = (float *)dev_workspace;
     p.part_ml = (float2 *)(p.part_o + (size_t)pl.splits * n_tokens * n_heads * d.head_dim);
     const dim3 grid((unsigned)grid_x, d.n_seqs);
-    if (d.head_dim == 128) {
-        if (pl.few)
-            hipLaunchKernelGGL((lvx_kv4_attention_kernel<128, 1, 1, 4>), grid, dim3(256), 0, (hipStream_t)stream, p);
-        else
-            hipLaunchKernelGGL((lvx_kv4_attention_kernel<128, 2, 4, 1>), grid, dim3(256), 0, (hipStream_t)stream, p);
-    } else {
-        if (pl.few)
-            hipLaunchKernelGGL((lvx_kv4_attention_kernel<64, 1, 1, 4>), grid, dim3(256), 0, (hipStream_t)stream, p);
-        else
-            hipLaunchKernelGGL((lvx_kv4_attention_kernel<64, 2, 4, 1>), grid, dim3(256), 0, (hipStream_t)stream, p);
-    }
+    d.head_dim == 128 ? attn_launch<128>(pl, p, grid, (hipStream_t)stream) : attn_launch<64>(pl, p, grid, (hipStream_t)stream);
     LVX_CHECK_HIP(hipGetLastError());
     if (pl.splits > 1) {
         const dim3 cgrid((unsigned)(((int64_t)max_tokens * n_heads + 3) / 4), d.n_seqs);
