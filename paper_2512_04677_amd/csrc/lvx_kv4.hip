@@ -210,6 +210,16 @@ struct attn_args_t {
     float2 *part_ml; // [split][token row][head]: reference (log2) and sum
 };
 
+// f over the four lanes that share a query (16 apart), in all of them
+template <typename F>
+__device__ __forceinline__ float across(float v, F f) {
+    const uint32_t u = __float_as_uint(v);
+    const auto a = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    const uint32_t w = __float_as_uint(f(__uint_as_float(a[0]), __uint_as_float(a[1])));
+    const auto b = __builtin_amdgcn_permlane16_swap(w, w, false, false);
+    return f(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
 // Rows of a workgroup: (token, head of the group) pairs of one sequence and kv head, row = token * group + head, 16 RB per wave, WR waves side by side;
 // WK waves share the keys, every WK-th tile each.
 template <int D, int RB, int WR, int WK>
@@ -218,7 +228,7 @@ __global__ void __launch_bounds__(64 * WR * WK, 2) lvx_kv4_attention_kernel(attn
     constexpr int CB = D / 16, KS = D / 32;  // channel blocks, steps of 32 channels
     constexpr int SLOT = RB * (CB * 4 + 2);  // floats a lane leaves for the joining
     __shared__ float join[WK > 1 ? WR * (WK - 1) * SLOT * 64 : 1];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wr = wave % WR, wk = wave / WR;
     const int r = lane & 15, g = lane >> 4;
     const int head = blockIdx.x % p.kv_heads, rt = (blockIdx.x / p.kv_heads) % p.row_tiles, split = blockIdx.x / p.kv_heads / p.row_tiles;
@@ -228,19 +238,17 @@ __global__ void __launch_bounds__(64 * WR * WK, 2) lvx_kv4_attention_kernel(attn
     if (rt * 16 * RB * WR >= n_rows) return;
 
     // this lane's rows: token, head and the number of keys they see
-    int64_t row_at[RB];
-    int seen[RB], head_of[RB];
+    int seen[RB];
     const int row0 = (rt * WR + wr) * 16 * RB;
     bf16x8_t q[RB][KS];
 #pragma unroll
     for (int b = 0; b < RB; ++b) {
         const int row = row0 + 16 * b + r;
         const int i = row < n_rows ? row / p.group : sp.n - 1;
-        head_of[b] = head * p.group + (row < n_rows ? row % p.group : 0);
-        row_at[b] = sp.first + i;
+        const int head_of = head * p.group + (row < n_rows ? row % p.group : 0);
         seen[b] = p.causal ? sp.count - (sp.n - 1 - i) : sp.count;
         seen[b] = row < n_rows && seen[b] > 0 ? seen[b] : 0;
-        const uint4 *src = reinterpret_cast<const uint4 *>(p.q + row_at[b] * p.ld_q + head_of[b] * D + (D / 4) * g);
+        const uint4 *src = reinterpret_cast<const uint4 *>(p.q + (int64_t)(sp.first + i) * p.ld_q + head_of * D + (D / 4) * g);
 #pragma unroll
         for (int j = 0; j < KS; ++j) {
             const uint4 v = src[j];
@@ -299,7 +307,6 @@ __global__ void __launch_bounds__(64 * WR * WK, 2) lvx_kv4_attention_kernel(attn
                 for (int b = 0; b < RB; ++b) x[b][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, q[b][j], x[b][kb], 0, 0, 0);
             }
         }
-        if (t + WK < t1) load_keys(t + WK);
         // softmax; lane's keys: 32 (kb / 2) + 8 g + 4 (kb % 2) + i
         const bool masked = TILE * (t + 1) > least;
         bf16x8_t pf[RB][2];
@@ -338,8 +345,7 @@ __global__ void __launch_bounds__(64 * WR * WK, 2) lvx_kv4_attention_kernel(attn
             auto maximum = [&]() {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) m = fmaxf(m, y[i]);
-                m = fmaxf(m, __shfl_xor(m, 16));
-                m = fmaxf(m, __shfl_xor(m, 32));
+                m = across(m, [](float a, float b) { return fmaxf(a, b); });
             };
             exponents();
             if (RUNNING) {
@@ -377,6 +383,7 @@ __global__ void __launch_bounds__(64 * WR * WK, 2) lvx_kv4_attention_kernel(attn
 #pragma unroll
             for (int i = 0; i < 16; ++i) pf[b][i >> 3][i & 7] = (__bf16)z[i];
         }
+        if (t + WK < t1) load_keys(t + WK);
         // outputs, transposed: a lane has four channels of each block for its query
 #pragma unroll
         for (int c2 = 0; c2 < CB / 2; ++c2) {
@@ -392,8 +399,7 @@ __global__ void __launch_bounds__(64 * WR * WK, 2) lvx_kv4_attention_kernel(attn
     }
 #pragma unroll
     for (int b = 0; b < RB; ++b) {
-        sum[b] += __shfl_xor(sum[b], 16);
-        sum[b] += __shfl_xor(sum[b], 32);
+        sum[b] = across(sum[b], [](float a, float b) { return a + b; });
     }
 
     // the waves that shared the keys: their results go to one, which adds them in their order
@@ -430,15 +436,18 @@ __global__ void __launch_bounds__(64 * WR * WK, 2) lvx_kv4_attention_kernel(attn
     }
 #pragma unroll
     for (int b = 0; b < RB; ++b) {
-        if (row0 + 16 * b + r >= n_rows) continue;
+        const int row = row0 + 16 * b + r;
+        if (row >= n_rows) continue;
+        const int64_t token = sp.first + row / p.group;
+        const int head_of = head * p.group + row % p.group;
         if (p.splits > 1) {
-            const int64_t at = ((int64_t)split * p.batch.n_tokens + row_at[b]) * p.n_heads + head_of[b];
+            const int64_t at = ((int64_t)split * p.batch.n_tokens + token) * p.n_heads + head_of;
 #pragma unroll
             for (int c = 0; c < CB; ++c) *reinterpret_cast<f32x4_t *>(p.part_o + at * D + 16 * c + 4 * g) = o[b][c];
             if (g == 0) p.part_ml[at] = make_float2(ref[b], sum[b]);
         } else {
             const float inv = seen[b] > 0 ? 1.0f / sum[b] : 0.f;  // a row that sees no key is zero
-            bf16_t *dst = p.out + row_at[b] * p.ld_out + head_of[b] * D + 4 * g;
+            bf16_t *dst = p.out + token * p.ld_out + head_of * D + 4 * g;
 #pragma unroll
             for (int c = 0; c < CB; ++c)
                 *reinterpret_cast<uint2 *>(dst + 16 * c) =
