@@ -321,11 +321,12 @@ __global__ void __launch_bounds__(64 * WR * WK, 2) lvx_kv4_attention_kernel(attn
 #pragma unroll
                     for (int i = 0; i < 4; ++i) y[4 * kb + i] = x[b][kb][i] * p.scale_log2 - base;
                 if (masked) {
+                    const int left = seen[b] - TILE * t - 8 * g;
 #pragma unroll
                     for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
-                            if (TILE * t + 32 * (kb >> 1) + 8 * g + 4 * (kb & 1) + i >= seen[b]) y[4 * kb + i] = -INFINITY;
+                            if (left <= 32 * (kb >> 1) + 4 * (kb & 1) + i) y[4 * kb + i] = -INFINITY;
                 }
             };
             auto powers = [&]() {
@@ -381,7 +382,11 @@ __global__ void __launch_bounds__(64 * WR * WK, 2) lvx_kv4_attention_kernel(attn
                 for (int i = 0; i < 16; ++i) z[i] = y[i] == 0.f ? 0.f : z[i];
             }
 #pragma unroll
-            for (int i = 0; i < 16; ++i) pf[b][i >> 3][i & 7] = (__bf16)z[i];
+            for (int h = 0; h < 2; ++h) {
+                const uint4 v = make_uint4(pack_bf16x2(z[8 * h], z[8 * h + 1]), pack_bf16x2(z[8 * h + 2], z[8 * h + 3]), pack_bf16x2(z[8 * h + 4], z[8 * h + 5]),
+                                           pack_bf16x2(z[8 * h + 6], z[8 * h + 7]));
+                pf[b][h] = *reinterpret_cast<const bf16x8_t *>(&v);
+            }
         }
         if (t + WK < t1) load_keys(t + WK);
         // outputs, transposed: a lane has four channels of each block for its query
