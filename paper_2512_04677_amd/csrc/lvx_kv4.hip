@@ -226,8 +226,8 @@ template <int D, int RB, int WR, int WK>
 __global__ void __launch_bounds__(64 * WR * WK, 2) lvx_kv4_attention_kernel(attn_args_t p) {
     typedef tile_t<D> T;
     constexpr int CB = D / 16, KS = D / 32;  // channel blocks, steps of 32 channels
-    constexpr int SLOT = RB * (CB * 4 + 2);  // floats a lane leaves for the joining
-    __shared__ float join[WK > 1 ? WR * (WK - 1) * SLOT * 64 : 1];
+    __shared__ f32x4_t join_o[WK > 1 ? WR * WK * RB * CB * 64 : 1];
+    __shared__ float2 join_ml[WK > 1 ? WR * WK * RB * 16 : 1];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wr = wave % WR, wk = wave / WR;
     const int r = lane & 15, g = lane >> 4;
@@ -307,6 +307,8 @@ __global__ void __launch_bounds__(64 * WR * WK, 2) lvx_kv4_attention_kernel(attn
                 for (int b = 0; b < RB; ++b) x[b][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, q[b][j], x[b][kb], 0, 0, 0);
             }
         }
+        // Registers bound how far ahead the next keys are requested: at once where a wave has one block of rows or the keys are shared, else when the scores are done with.
+        if (WK > 1 && t + WK < t1) load_keys(t + WK);
         // softmax; lane's keys: 32 (kb / 2) + 8 g + 4 (kb % 2) + i
         const bool masked = TILE * (t + 1) > least;
         bf16x8_t pf[RB][2];
@@ -388,7 +390,7 @@ __global__ void __launch_bounds__(64 * WR * WK, 2) lvx_kv4_attention_kernel(attn
                 pf[b][h] = *reinterpret_cast<const bf16x8_t *>(&v);
             }
         }
-        if (t + WK < t1) load_keys(t + WK);
+        if (WK == 1 && t + WK < t1) load_keys(t + WK);
         // outputs, transposed: a lane has four channels of each block for its query
 #pragma unroll
         for (int c2 = 0; c2 < CB / 2; ++c2) {
@@ -407,56 +409,59 @@ __global__ void __launch_bounds__(64 * WR * WK, 2) lvx_kv4_attention_kernel(attn
         sum[b] = across(sum[b], [](float a, float b) { return a + b; });
     }
 
-    // the waves that shared the keys: their results go to one, which adds them in their order
+    // The waves that shared the keys leave their results to each other: every wave joins, in the order of the waves, and stores its share of the channel blocks.
     if (WK > 1) {
-        if (wk > 0) {
-            float *at = join + ((wr * (WK - 1) + wk - 1) * SLOT) * 64 + lane;
 #pragma unroll
-            for (int b = 0; b < RB; ++b) {
-                at[(b * (CB * 4 + 2)) * 64] = ref[b];
-                at[(b * (CB * 4 + 2) + 1) * 64] = sum[b];
+        for (int b = 0; b < RB; ++b) {
+            if (g == 0) join_ml[((wr * WK + wk) * RB + b) * 16 + r] = make_float2(ref[b], sum[b]);
 #pragma unroll
-                for (int c = 0; c < CB; ++c)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) at[(b * (CB * 4 + 2) + 2 + 4 * c + i) * 64] = o[b][c][i];
-            }
+            for (int c = 0; c < CB; ++c) join_o[(((wr * WK + wk) * RB + b) * CB + c) * 64 + lane] = o[b][c];
         }
         __syncthreads();
-        if (wk > 0) return;
-        for (int k = 1; k < WK; ++k) {
-            const float *at = join + ((wr * (WK - 1) + k - 1) * SLOT) * 64 + lane;
-#pragma unroll
-            for (int b = 0; b < RB; ++b) {
-                const float other = at[(b * (CB * 4 + 2)) * 64];
-                const float next = fmaxf(ref[b], other), base = next == -INFINITY ? 0.f : next;
-                const float mine = __builtin_amdgcn_exp2f(ref[b] - base), its = __builtin_amdgcn_exp2f(other - base);
-                ref[b] = next;
-                sum[b] = sum[b] * mine + at[(b * (CB * 4 + 2) + 1) * 64] * its;
-#pragma unroll
-                for (int c = 0; c < CB; ++c)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) o[b][c][i] = o[b][c][i] * mine + at[(b * (CB * 4 + 2) + 2 + 4 * c + i) * 64] * its;
-            }
-        }
     }
 #pragma unroll
     for (int b = 0; b < RB; ++b) {
         const int row = row0 + 16 * b + r;
-        if (row >= n_rows) continue;
+        const bool there = row < n_rows;
         const int64_t token = sp.first + row / p.group;
         const int head_of = head * p.group + row % p.group;
-        if (p.splits > 1) {
-            const int64_t at = ((int64_t)split * p.batch.n_tokens + token) * p.n_heads + head_of;
+        float factor[WK];
+        if (WK > 1) {
+            ref[b] = -INFINITY, sum[b] = 0;
+            float2 ml[WK];
 #pragma unroll
-            for (int c = 0; c < CB; ++c) *reinterpret_cast<f32x4_t *>(p.part_o + at * D + 16 * c + 4 * g) = o[b][c];
-            if (g == 0) p.part_ml[at] = make_float2(ref[b], sum[b]);
-        } else {
-            const float inv = seen[b] > 0 ? 1.0f / sum[b] : 0.f;  // a row that sees no key is zero
-            bf16_t *dst = p.out + token * p.ld_out + head_of * D + 4 * g;
+            for (int k = 0; k < WK; ++k) {
+                ml[k] = join_ml[((wr * WK + k) * RB + b) * 16 + r];
+                ref[b] = fmaxf(ref[b], ml[k].x);
+            }
 #pragma unroll
-            for (int c = 0; c < CB; ++c)
-                *reinterpret_cast<uint2 *>(dst + 16 * c) =
-                    make_uint2(pack_bf16x2(o[b][c][0] * inv, o[b][c][1] * inv), pack_bf16x2(o[b][c][2] * inv, o[b][c][3] * inv));
+            for (int k = 0; k < WK; ++k) {
+                factor[k] = __builtin_amdgcn_exp2f(ml[k].x - (ref[b] == -INFINITY ? 0.f : ref[b]));
+                sum[b] += ml[k].y * factor[k];
+            }
+        }
+        const int64_t at = ((int64_t)split * p.batch.n_tokens + token) * p.n_heads + head_of;
+        const float inv = seen[b] > 0 ? 1.0f / sum[b] : 0.f;  // a row that sees no key is zero
+        if (p.splits > 1 && there && g == 0 && wk == 0) p.part_ml[at] = make_float2(ref[b], sum[b]);
+#pragma unroll
+        for (int c = 0; c < CB; ++c) {
+            if (WK > 1 && (b * CB + c) % WK != wk) continue;
+            f32x4_t v = o[b][c];
+            if (WK > 1) {
+                v = {0, 0, 0, 0};
+#pragma unroll
+                for (int k = 0; k < WK; ++k) {
+                    const f32x4_t its = join_o[(((wr * WK + k) * RB + b) * CB + c) * 64 + lane];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[i] += its[i] * factor[k];
+                }
+            }
+            if (!there) continue;
+            if (p.splits > 1)
+                *reinterpret_cast<f32x4_t *>(p.part_o + at * D + 16 * c + 4 * g) = v;
+            else
+                *reinterpret_cast<uint2 *>(p.out + token * p.ld_out + head_of * D + 16 * c + 4 * g) =
+                    make_uint2(pack_bf16x2(v[0] * inv, v[1] * inv), pack_bf16x2(v[2] * inv, v[3] * inv));
         }
     }
 }
@@ -472,16 +477,31 @@ __global__ void __launch_bounds__(256) lvx_kv4_combine_kernel(attn_args_t p) {
     if (row >= sp.n * p.n_heads) return;
     const int i = row / p.n_heads, head = row % p.n_heads;
     const int64_t at0 = (int64_t)(sp.first + i) * p.n_heads + head, step = (int64_t)p.batch.n_tokens * p.n_heads;
-    float ref = -INFINITY;
-    for (int k = 0; k < p.splits; ++k) ref = fmaxf(ref, p.part_ml[at0 + k * step].x);
-    const float base = ref == -INFINITY ? 0.f : ref;
-    float sum = 0, o[C] = {};
-    for (int k = 0; k < p.splits; ++k) {
-        const float2 ml = p.part_ml[at0 + k * step];
-        const float f = __builtin_amdgcn_exp2f(ml.x - base);
-        sum += ml.y * f;
+    // lane k has range k's reference and sum
+    const float2 ml = lane < p.splits ? p.part_ml[at0 + lane * step] : make_float2(-INFINITY, 0.f);
+    float ref = ml.x;
 #pragma unroll
-        for (int c = 0; c < C; ++c) o[c] += p.part_o[(at0 + k * step) * D + C * lane + c] * f;
+    for (int d = 32; d >= 1; d >>= 1) ref = fmaxf(ref, __shfl_xor(ref, d));
+    const float factor = __builtin_amdgcn_exp2f(ml.x - (ref == -INFINITY ? 0.f : ref));
+    float sum = ml.y * factor;
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) sum += __shfl_xor(sum, d);
+    float o[C] = {};
+    const float *src = p.part_o + at0 * D + C * lane;
+    for (int k0 = 0; k0 < p.splits; k0 += 8) {
+        float x[8][C];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const float *from = src + (k0 + k < p.splits ? k0 + k : 0) * step * D;
+#pragma unroll
+            for (int c = 0; c < C; ++c) x[k][c] = from[c];
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const float f = k0 + k < p.splits ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(factor), k0 + k)) : 0.f;
+#pragma unroll
+            for (int c = 0; c < C; ++c) o[c] += k0 + k < p.splits ? x[k][c] * f : 0.f;
+        }
     }
     const int seen = p.causal ? sp.count - (sp.n - 1 - i) : sp.count;
     const float inv = seen > 0 ? 1.0f / sum : 0.f;
@@ -628,8 +648,9 @@ attn_plan_t attn_plan(const lvx_kv4_desc_t &d, int n_heads, int max_tokens) {
     pl.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
     pl.row_tiles = (int)((rows + pl.rows - 1) / pl.rows);
     const int64_t groups = (int64_t)pl.row_tiles * d.n_kv_heads * d.n_seqs;
-    int64_t splits = groups > 0 ? 1024 / groups : 1;
-    const int64_t most = d.max_keys / 512;
+    const bool shared = pl.rows <= 32;  // eight waves share the keys
+    int64_t splits = groups > 0 ? 512 / groups : 1;
+    const int64_t most = d.max_keys / (shared ? 1024 : 512);
     splits = splits < most ? splits : most;
     splits = splits < MAX_SPLITS ? splits : MAX_SPLITS;
     pl.splits = (int)(splits > 1 ? splits : 1);
@@ -639,9 +660,9 @@ attn_plan_t attn_plan(const lvx_kv4_desc_t &d, int n_heads, int max_tokens) {
 template <int D>
 void attn_launch(const attn_plan_t &pl, const attn_args_t &p, dim3 grid, hipStream_t stream) {
     if (pl.rows == 16)
-        hipLaunchKernelGGL((lvx_kv4_attention_kernel<D, 1, 1, 4>), grid, dim3(256), 0, stream, p);
+        hipLaunchKernelGGL((lvx_kv4_attention_kernel<D, 1, 1, 8>), grid, dim3(512), 0, stream, p);
     else if (pl.rows == 32)
-        hipLaunchKernelGGL((lvx_kv4_attention_kernel<D, 2, 1, 4>), grid, dim3(256), 0, stream, p);
+        hipLaunchKernelGGL((lvx_kv4_attention_kernel<D, 2, 1, 8>), grid, dim3(512), 0, stream, p);
     else if (pl.rows == 64)
         hipLaunchKernelGGL((lvx_kv4_attention_kernel<D, 2, 2, 2>), grid, dim3(256), 0, stream, p);
     else
@@ -666,8 +687,9 @@ extern "C" size_t lvx_kv4_attention_workspace_bytes(const lvx_kv4_t *cache, int3
     uint64_t n = 256;
     for (int32_t t = 1; t <= max_tokens; ++t) {
         const uint64_t its = attn_scratch(cache->desc, n_heads, t);
-        if (its == 0) break;  // from here on too
         n = n > its ? n : its;
+        const attn_plan_t pl = attn_plan(cache->desc, n_heads, t);
+        if (pl.rows == 128 && pl.splits == 1) break;  // and none is from here on
     }
     return (size_t)n;
 }
