@@ -78,81 +78,117 @@ struct append_args_t {
     int32_t kv_heads, max_keys;
 };
 
-// A wave quantises eight aligned keys of one head: keys of a word of V are never shared between waves.
-template <int D>
+// maximum over a row of 16 lanes, in all of them
+__device__ __forceinline__ uint32_t row_max(uint32_t v) {
+#define LVX_ROR(n_)                                                                                     \
+    {                                                                                                   \
+        const uint32_t o = (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x120 + n_, 0xf, 0xf, false);     \
+        v = v > o ? v : o;                                                                              \
+    }
+    LVX_ROR(8) LVX_ROR(4) LVX_ROR(2) LVX_ROR(1)
+#undef LVX_ROR
+    return v;
+}
+__device__ __forceinline__ uint32_t swap_max(uint32_t a, uint32_t b, bool halves) {  // lanes of the lower half (even rows): a's maximum over the halves (row pairs), the others: b's
+    if (halves) {
+        const auto r = __builtin_amdgcn_permlane32_swap(a, b, false, false);
+        return r[0] > r[1] ? r[0] : r[1];
+    }
+    const auto r = __builtin_amdgcn_permlane16_swap(a, b, false, false);
+    return r[0] > r[1] ? r[0] : r[1];
+}
+
+// A wave quantises 8 NG aligned keys of one head: the keys of a word of V are never shared between waves.
+template <int D, int NG>
 __global__ void __launch_bounds__(256) lvx_kv4_append_kernel(append_args_t p) {
     typedef tile_t<D> T;
     const int lane = threadIdx.x & 63;
-    const int s = blockIdx.y, head = blockIdx.z * 4 + (threadIdx.x >> 6);
+    const int s = blockIdx.y, head = blockIdx.z * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (head >= p.kv_heads) return;
     const int c_raw = p.batch.counts[s];
     const span_t sp = span_of(p.batch, s, p.max_keys);
     const int64_t pos0 = (int64_t)c_raw - sp.n;  // position of the first token, before clipping
     const int64_t lo = pos0 > 0 ? pos0 : 0, hi = c_raw < p.max_keys ? c_raw : p.max_keys;
-    const int64_t key0 = (lo & ~7ll) + 8ll * blockIdx.x;
-    if (key0 >= hi || sp.n <= 0) return;
-    uint8_t *rec = p.base + s * p.seq_stride + head * p.head_stride + (key0 / TILE) * T::BYTES;
-    const int kt = (int)(key0 % TILE);
+    const int64_t first = (lo & ~(8ll * NG - 1)) + 8ll * NG * blockIdx.x;
+    if (first >= hi || sp.n <= 0) return;
+    uint8_t *rec = p.base + s * p.seq_stride + head * p.head_stride + (first / TILE) * T::BYTES;
+    const int kt0 = (int)(first % TILE);
 
     // keys: a thread per key and group of 32 channels
-    if (lane < 8 * (D / 32)) {
+    if (lane < 8 * NG * (D / 32)) {
         const int i = lane / (D / 32), grp = lane % (D / 32);
-        const int64_t key = key0 + i;
+        const int64_t key = first + i;
         if (key >= lo && key < hi) {
             const uint4 *src = reinterpret_cast<const uint4 *>(p.k + (sp.first + (key - pos0)) * p.ld + head * D + 32 * grp);
             uint4 x[4];
             uint32_t m = 0;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                x[j] = src[j];
-                m = lvx_amax_bf16x2(lvx_amax_bf16x2(lvx_amax_bf16x2(lvx_amax_bf16x2(m, x[j].x), x[j].y), x[j].z), x[j].w);
-            }
+            for (int j = 0; j < 4; ++j) x[j] = src[j];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) m = lvx_amax_bf16x2(lvx_amax_bf16x2(lvx_amax_bf16x2(lvx_amax_bf16x2(m, x[j].x), x[j].y), x[j].z), x[j].w);
             const uint32_t byte = lvx_fp4_group_byte(m);
             const float scale = lvx_e8m0_f32(byte);
             uint32_t w[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) w[j] = byte == 255 ? 0 : lvx_bf16x8_fp4(x[j].x, x[j].y, x[j].z, x[j].w, scale);
-            *reinterpret_cast<uint2 *>(rec + T::k_piece(kt + i, grp, 0)) = make_uint2(w[0], w[1]);
-            *reinterpret_cast<uint2 *>(rec + T::k_piece(kt + i, grp, 1)) = make_uint2(w[2], w[3]);
-            rec[T::k_scale(kt + i, grp)] = (uint8_t)byte;
+            *reinterpret_cast<uint2 *>(rec + T::k_piece(kt0 + i, grp, 0)) = make_uint2(w[0], w[1]);
+            *reinterpret_cast<uint2 *>(rec + T::k_piece(kt0 + i, grp, 1)) = make_uint2(w[2], w[3]);
+            rec[T::k_scale(kt0 + i, grp)] = (uint8_t)byte;
         }
     }
 
-    // values: a lane has D / 64 channels of all eight keys
+    // values: a lane has D / 64 channels of all keys
     constexpr int C = D / 64;
-    uint32_t word[C];
+    uint32_t x[NG][8];
 #pragma unroll
-    for (int c = 0; c < C; ++c) word[c] = 0;
-    uint32_t keep = 0;  // nibbles of keys that this call does not write
+    for (int n = 0; n < NG; ++n)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int64_t key = key0 + i;
-        if (key < lo || key >= hi) {
-            keep |= 15u << (4 * i);
-            continue;
+        for (int i = 0; i < 8; ++i) {
+            const int64_t key = first + 8 * n + i;
+            x[n][i] = 0;
+            if (key < lo || key >= hi) continue;
+            const bf16_t *src = p.v + (sp.first + (key - pos0)) * p.ld + head * D + C * lane;
+            x[n][i] = C == 2 ? *reinterpret_cast<const uint32_t *>(src) : (uint32_t)*reinterpret_cast<const uint16_t *>(src);
         }
-        const bf16_t *src = p.v + (sp.first + (key - pos0)) * p.ld + head * D + C * lane;
-        const uint32_t x = C == 2 ? *reinterpret_cast<const uint32_t *>(src) : (uint32_t)*reinterpret_cast<const uint16_t *>(src);
-        uint32_t m = lvx_amax_bf16x2(0, x);
 #pragma unroll
-        for (int d = 32; d >= 1; d >>= 1) {
-            const uint32_t o = (uint32_t)__shfl_xor((int)m, d);
-            m = m > o ? m : o;
+    for (int n = 0; n < NG; ++n) {
+        const int64_t key0 = first + 8 * n;
+        const int kt = kt0 + 8 * n;
+        if (key0 >= hi || key0 + 8 <= lo) continue;
+        // the eight maxima over the wave: over its halves, its pairs of rows, its rows of 16 lanes
+        uint32_t m[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m[i] = lvx_amax_bf16x2(0, x[n][i]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) m[i] = swap_max(m[2 * i], m[2 * i + 1], true);  // lower half: key 2 i, upper: 2 i + 1
+#pragma unroll
+        for (int i = 0; i < 2; ++i) m[i] = row_max(swap_max(m[2 * i], m[2 * i + 1], false));  // even rows: keys 4 i, 4 i + 1, odd rows: 4 i + 2, 4 i + 3
+        uint32_t word[C];
+#pragma unroll
+        for (int c = 0; c < C; ++c) word[c] = 0;
+        uint32_t keep = 0;  // nibbles of keys that this call does not write
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (key0 + i < lo || key0 + i >= hi) {
+                keep |= 15u << (4 * i);
+                continue;
+            }
+            const uint32_t most = __builtin_amdgcn_readlane(m[i >> 2], 32 * (i & 1) + 16 * ((i >> 1) & 1));
+            const uint32_t sb = pack_bf16x2(__uint_as_float(most) / 6.0f, 0.f) & 0xffffu;
+            float scale = bf16_bits_to_f32(sb);
+            scale = scale < 0x1p-120f ? 0x1p-120f : scale;
+            // x / scale has more than the bits that separate it from a border between two codes, so the division's rounding decides nothing
+            const uint32_t code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0, bf16_lo(x[n][i]) / scale, bf16_hi(x[n][i]) / scale, 1.0f, 0);
+#pragma unroll
+            for (int c = 0; c < C; ++c) word[c] |= ((code >> (4 * c)) & 15u) << (4 * i);
+            if (lane == 0) *reinterpret_cast<uint16_t *>(rec + T::v_scale(kt + i)) = (uint16_t)(__float_as_uint(scale) >> 16);
         }
-        const uint32_t sb = pack_bf16x2(__uint_as_float(m) / 6.0f, 0.f) & 0xffffu;
-        float scale = bf16_bits_to_f32(sb);
-        scale = scale < 0x1p-120f ? 0x1p-120f : scale;
-        // x / scale has more than the bits that separate it from a border between two codes, so the division's rounding decides nothing
-        const uint32_t code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0, bf16_lo(x) / scale, bf16_hi(x) / scale, 1.0f, 0);
 #pragma unroll
-        for (int c = 0; c < C; ++c) word[c] |= ((code >> (4 * c)) & 15u) << (4 * i);
-        if (lane == 0) *reinterpret_cast<uint16_t *>(rec + T::v_scale(kt + i)) = (uint16_t)(__float_as_uint(scale) >> 16);
-    }
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-        uint32_t *dst = reinterpret_cast<uint32_t *>(rec + T::v_word(kt, C * lane + c));
-        if (keep != 0) word[c] |= *dst & keep;
-        *dst = word[c];
+        for (int c = 0; c < C; ++c) {
+            uint32_t *dst = reinterpret_cast<uint32_t *>(rec + T::v_word(kt, C * lane + c));
+            if (keep != 0) word[c] |= *dst & keep;
+            *dst = word[c];
+        }
     }
 }
 
@@ -165,35 +201,50 @@ struct gather_args_t {
     int32_t first_key, n_keys, kv_heads, max_keys;
 };
 
-// A thread reads eight channels of a key, or writes zeros behind the sequence's last key.
+// A thread reads eight channels of eight aligned keys, or writes zeros behind the sequence's last key.
 template <int D>
 __global__ void __launch_bounds__(256) lvx_kv4_gather_kernel(gather_args_t p) {
     typedef tile_t<D> T;
     const int s = blockIdx.y, per_key = p.kv_heads * (D / 8);
-    const int64_t total = (int64_t)p.n_keys * per_key;
+    const int g0 = p.first_key / 8, groups = (p.first_key + p.n_keys + 7) / 8 - g0;
+    const int64_t total = (int64_t)groups * per_key;
     const int count = p.counts[s] < p.max_keys ? p.counts[s] : p.max_keys;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-        const int64_t j = i / per_key;
-        const int e = (int)(i % per_key), head = e / (D / 8), c0 = 8 * (e % (D / 8));
-        const int64_t key = p.first_key + j;
-        uint4 ko = make_uint4(0, 0, 0, 0), vo = ko;
-        if (key < count) {
-            const uint8_t *rec = p.base + s * p.seq_stride + head * p.head_stride + (key / TILE) * T::BYTES;
-            const int kt = (int)(key % TILE), grp = c0 / 32, in = c0 % 32;
-            const uint32_t kw = *reinterpret_cast<const uint32_t *>(rec + T::k_piece(kt, grp, in / 16) + (in % 16) / 2);
-            const bf16x8_t kx = lvx_fp4x8_bf16(kw, lvx_e8m0_f32(rec[T::k_scale(kt, grp)]));
-            ko = *reinterpret_cast<const uint4 *>(&kx);
-            const float vs = bf16_bits_to_f32(*reinterpret_cast<const uint16_t *>(rec + T::v_scale(kt)));
-            uint32_t vw = 0;
+        const int e = (int)(i % per_key), head = e / (D / 8), c0 = 8 * (e % (D / 8)), grp = c0 / 32, in = c0 % 32;
+        const int key0 = 8 * (g0 + (int)(i / per_key)), kt = key0 % TILE;
+        uint32_t kw[8], vw[8], kb[8];
+        uint4 vs = make_uint4(0, 0, 0, 0);
+        if (key0 < count) {
+            const uint8_t *rec = p.base + s * p.seq_stride + head * p.head_stride + (int64_t)(key0 / TILE) * T::BYTES;
 #pragma unroll
-            for (int c = 0; c < 8; ++c) vw |= ((*reinterpret_cast<const uint32_t *>(rec + T::v_word(kt & ~7, c0 + c)) >> (4 * (kt & 7))) & 15u) << (4 * c);
-            const bf16x8_t vx = lvx_fp4x8_bf16(vw, 1.0f);
-            vo.x = pack_bf16x2((float)vx[0] * vs, (float)vx[1] * vs), vo.y = pack_bf16x2((float)vx[2] * vs, (float)vx[3] * vs);
-            vo.z = pack_bf16x2((float)vx[4] * vs, (float)vx[5] * vs), vo.w = pack_bf16x2((float)vx[6] * vs, (float)vx[7] * vs);
+            for (int j = 0; j < 8; ++j) {
+                kw[j] = *reinterpret_cast<const uint32_t *>(rec + T::k_piece(kt + j, grp, in / 16) + (in % 16) / 2);
+                kb[j] = rec[T::k_scale(kt + j, grp)];
+                vw[j] = *reinterpret_cast<const uint32_t *>(rec + T::v_word(kt, c0 + j));
+            }
+            vs = *reinterpret_cast<const uint4 *>(rec + T::v_scale(kt));
         }
-        const int64_t at = ((int64_t)s * p.n_keys + j) * p.ld + head * D + c0;
-        *reinterpret_cast<uint4 *>(p.k + at) = ko;
-        *reinterpret_cast<uint4 *>(p.v + at) = vo;
+        const uint32_t vsw[4] = {vs.x, vs.y, vs.z, vs.w};
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int key = key0 + j;
+            if (key < p.first_key || key >= p.first_key + p.n_keys) continue;
+            uint4 ko = make_uint4(0, 0, 0, 0), vo = ko;
+            if (key < count) {
+                const bf16x8_t kx = lvx_fp4x8_bf16(kw[j], lvx_e8m0_f32(kb[j]));
+                ko = *reinterpret_cast<const uint4 *>(&kx);
+                uint32_t w = 0;
+#pragma unroll
+                for (int c = 0; c < 8; ++c) w |= ((vw[c] >> (4 * j)) & 15u) << (4 * c);
+                const float f = (j & 1) ? bf16_hi(vsw[j >> 1]) : bf16_lo(vsw[j >> 1]);
+                const bf16x8_t vx = lvx_fp4x8_bf16(w, 1.0f);
+                vo.x = pack_bf16x2((float)vx[0] * f, (float)vx[1] * f), vo.y = pack_bf16x2((float)vx[2] * f, (float)vx[3] * f);
+                vo.z = pack_bf16x2((float)vx[4] * f, (float)vx[5] * f), vo.w = pack_bf16x2((float)vx[6] * f, (float)vx[7] * f);
+            }
+            const int64_t at = ((int64_t)s * p.n_keys + key - p.first_key) * p.ld + head * D + c0;
+            *reinterpret_cast<uint4 *>(p.k + at) = ko;
+            *reinterpret_cast<uint4 *>(p.v + at) = vo;
+        }
     }
 }
 
@@ -594,13 +645,13 @@ extern "C" lvx_status_t lvx_kv4_append(lvx_kv4_t *cache, int32_t layer, const vo
     p.k = (const bf16_t *)dev_k, p.v = (const bf16_t *)dev_v, p.ld = ld;
     p.batch = {dev_starts, dev_key_counts, max_tokens, n_tokens};
     p.kv_heads = d.n_kv_heads, p.max_keys = d.max_keys;
-    // max_tokens keys from any position on touch at most this many groups of eight
+    // max_tokens keys from any position on touch at most this many aligned groups; a wave takes two of eight keys where sequences bring that many
     const int64_t span = max_tokens < d.max_keys ? max_tokens : d.max_keys;
-    const dim3 grid((unsigned)((span + 14) / 8), d.n_seqs, (d.n_kv_heads + 3) / 4);
-    if (d.head_dim == 128)
-        hipLaunchKernelGGL(lvx_kv4_append_kernel<128>, grid, dim3(256), 0, (hipStream_t)stream, p);
-    else
-        hipLaunchKernelGGL(lvx_kv4_append_kernel<64>, grid, dim3(256), 0, (hipStream_t)stream, p);
+    const int per = max_tokens > 8 ? 16 : 8;
+    const dim3 grid((unsigned)((span + 2 * per - 2) / per), d.n_seqs, (d.n_kv_heads + 3) / 4);
+    auto *kernel = d.head_dim == 128 ? (per == 16 ? lvx_kv4_append_kernel<128, 2> : lvx_kv4_append_kernel<128, 1>)
+                                     : (per == 16 ? lvx_kv4_append_kernel<64, 2> : lvx_kv4_append_kernel<64, 1>);
+    hipLaunchKernelGGL(kernel, grid, dim3(256), 0, (hipStream_t)stream, p);
     LVX_CHECK_HIP(hipGetLastError());
     return LVX_OK;
 }
@@ -622,7 +673,7 @@ extern "C" lvx_status_t lvx_kv4_gather(const lvx_kv4_t *cache, int32_t layer, in
     p.k = (bf16_t *)dev_k_out, p.v = (bf16_t *)dev_v_out, p.ld = ld;
     p.counts = dev_key_counts;
     p.first_key = first_key, p.n_keys = n_keys, p.kv_heads = d.n_kv_heads, p.max_keys = d.max_keys;
-    const int64_t items = (int64_t)n_keys * d.n_kv_heads * (d.head_dim / 8);
+    const int64_t items = ((int64_t)n_keys + 14) / 8 * d.n_kv_heads * (d.head_dim / 8);
     const dim3 grid((unsigned)(items < 256 * 4096 ? (items + 255) / 256 : 4096), d.n_seqs);
     if (d.head_dim == 128)
         hipLaunchKernelGGL(lvx_kv4_gather_kernel<128>, grid, dim3(256), 0, (hipStream_t)stream, p);

@@ -151,7 +151,7 @@ __global__ void __launch_bounds__(T < 256 ? 256 : T) lvx_rmsnorm_residual_kernel
 
 template <bool F32, bool FP8>
 void launch(const norm_args_t &p, hipStream_t stream) {
-    if (p.chunks <= 64 * 4)
+    if (p.chunks <= 64 * 4 && p.n_tokens >= 2048)
         hipLaunchKernelGGL((lvx_rmsnorm_residual_kernel<64, 4, F32, FP8>), dim3((p.n_tokens + 3) / 4), dim3(256), 0, stream, p);
     else if (p.chunks <= 256 * 4)
         hipLaunchKernelGGL((lvx_rmsnorm_residual_kernel<256, 4, F32, FP8>), dim3(p.n_tokens), dim3(256), 0, stream, p);
