@@ -131,7 +131,7 @@ __device__ __forceinline__ void swap16(uint32_t &a, uint32_t &b) {  // odd rows 
     a = r[0], b = r[1];
 }
 
-constexpr int PANEL = 64;  // steps whose scales are held in LDS
+constexpr int PANEL = 48;  // steps whose scales a tile holds in LDS
 
 // ---- few rows: a wave per 16 NB columns and range of K -----------------------------------------------------------------
 // Bound by the weights' way from HBM.  A workgroup of blockDim.x / 64 waves owns 16 NB columns and 16 MB rows; the waves take units of U steps of 128 channels in turn.
@@ -254,171 +254,185 @@ __global__ void __launch_bounds__(512) lvx_fp4_few_kernel(fp4_args_t p) {
     }
 }
 
-// ---- many rows: tiles of 16 MB rows and 128 columns ---------------------------------------------------------------------
-// Bound by the matrix cores.  Eight waves: two beside each other over the columns (64 each, whose weights go straight into registers), four groups over K, every
-// fourth step each, with the rows of A in LDS, a step ahead.  A row of a stage is 128 (8 bits) or 256 bytes; its 16-byte chunk c lies at c ^ (row % 8 or 16), so that
-// the sixteen rows of an operand fall into different banks.
-template <int MODE, int MB>
+// ---- many rows: tiles of 32 MBW rows and 128 columns ---------------------------------------------------------------------
+// Bound by the matrix cores and the LDS.  Eight waves: two groups over K, every second pair of steps each, of two by two waves (half the rows, half the columns).  Rows
+// and weights come by direct loads to LDS, RING steps and a pair or two of steps ahead: a stage of the weights is a pair, because a weight row's 128 channels are half a
+// cache line and halves cost as much as lines.  A wave reads the next step's operands into registers while it multiplies this one's.  16-byte chunk c of a row of CH
+// chunks lies at c ^ (row % CH), so that the sixteen rows of an operand fall into different banks.
+template <int MODE, int MBW, int RING>
 __global__ void __launch_bounds__(512) lvx_fp4_tile_kernel(fp4_args_t p) {
-    constexpr int NB = 4, KG = 4, AV = MODE == A_BF16 ? 4 : 2, ROW = MODE == A_BF16 ? 256 : 128, CH = ROW / 16;
-    constexpr int STAGE = MB * 16 * ROW;
-    extern __shared__ char lds[];  // [KG][2][STAGE], then the partial sums
+    constexpr int NB = 4, AV = MODE == A_BF16 ? 4 : 2, ROW = MODE == A_BF16 ? 256 : 128, CH = ROW / 16, MT = 32 * MBW;
+    constexpr int A_STAGE = MT * ROW, W_STAGE = 128 * 128, A_PER = 1024 / ROW;  // A_PER: rows of an instruction
+    constexpr int DA = A_STAGE / 4096, DW = 4;                                  // requests of a wave per stage
+    extern __shared__ char lds[];  // [2][RING] stages of rows, [2][2] of weights, the scales; then the partial sums
+    uint32_t *scales = reinterpret_cast<uint32_t *>(lds + 2 * RING * A_STAGE + 4 * W_STAGE);  // [128][PANEL]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int nw = wave & 1, kg = wave >> 1;
+    const int kg = wave >> 2, mw = (wave >> 1) & 1, nw = wave & 1, in_group = wave & 3;
     const int r = lane & 15, g = lane >> 4;
-    const int n0 = blockIdx.x * 128 + nw * 64, m0 = blockIdx.y * 16 * MB;
-    __shared__ uint32_t scales[128 * (PANEL + 1)];
-    const uint8_t *w_row[NB];
+    const int n0 = blockIdx.x * 128, m0 = blockIdx.y * MT;
+    const int steps = (p.K + 127) / 128, rounds = (steps + 3) / 4;
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
+    const uint32_t lds_a = lds0 + kg * RING * A_STAGE, lds_w = lds0 + 2 * RING * A_STAGE + kg * 2 * W_STAGE;
+
+    // this wave's share of its group's requests: rows past the end repeat the last one (they are multiplied and not stored)
+    uint32_t a_off[DA], a_col[DA], w_off[DW], w_col[DW];
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-        const int n = n0 + 16 * b + r < p.N ? n0 + 16 * b + r : p.N - 1;
-        w_row[b] = p.W + n * p.ldw + 16 * g;
+    for (int i = 0; i < DA; ++i) {
+        const int row = (in_group * DA + i) * A_PER + lane / CH;
+        a_off[i] = (uint32_t)((m0 + row < p.M ? row : p.M - 1 - m0) * p.lda);
+        a_col[i] = (uint32_t)((lane % CH) ^ (row % CH));
     }
-    // this wave's half of the group's stage: row and chunk of each lane's 16 bytes per instruction
-    constexpr int DMAS = STAGE / 1024 / 2, ROWS_PER = 1024 / ROW;
-    uint32_t a_off[DMAS];
 #pragma unroll
-    for (int i = 0; i < DMAS; ++i) {
-        const int row = (nw * DMAS + i) * ROWS_PER + lane / CH;
-        const int m = m0 + row < p.M ? row : p.M - 1 - m0;
-        a_off[i] = (uint32_t)(m * p.lda);
+    for (int i = 0; i < DW; ++i) {
+        const int row = (in_group * DW + i) * 8 + lane / 8;
+        w_off[i] = (uint32_t)((n0 + row < p.N ? row : p.N - 1 - n0) * p.ldw);
+        w_col[i] = (uint32_t)((lane % 8) ^ (row % 8));
     }
     const char *a_base = p.A + (int64_t)m0 * p.lda;
-    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds + kg * 2 * STAGE + nw * (STAGE / 2);
-    f32x4_t acc[NB][MB];
+    const uint8_t *w_base = p.W + (int64_t)n0 * p.ldw;
+    // the group's j-th step: pairs kg, kg + 2, ... of two steps each
+    auto step = [&](int j) { return 2 * (kg + 2 * (j >> 1)) + (j & 1); };
+    // of the last stage, chunks behind K are not read: the row's first is, in their place, and not used
+    auto stage_a = [&](int j) {
+        const int t = step(j);
+        const uint32_t chunks = (uint32_t)((p.K - 128 * t) * (ROW / 128) / 16), to = lds_a + (j % RING) * A_STAGE;
+#pragma unroll
+        for (int i = 0; i < DA; ++i)
+            lvx_dma16(a_base, a_off[i] + (a_col[i] < chunks ? (uint32_t)t * ROW + 16 * a_col[i] : 0), to + (in_group * DA + i) * 1024);
+    };
+    auto stage_w = [&](int j) {  // of the pair that begins with step j
+        const int q = kg + 2 * (j >> 1);
+        const uint32_t chunks = (uint32_t)((p.K - 256 * q) / 32), to = lds_w + ((j >> 1) & 1) * W_STAGE;
+#pragma unroll
+        for (int i = 0; i < DW; ++i)
+            lvx_dma16(w_base, w_off[i] + (w_col[i] < chunks ? (uint32_t)q * 128 + 16 * w_col[i] : 0), to + (in_group * DW + i) * 1024);
+    };
+    // the scales of the PANEL steps (of both groups) from the group's step j on: 16 bytes = four steps of a column a piece
+    auto load_scales = [&](int j) {
+        const int b0 = 8 * j, row_bytes = p.K / LVX_FP4_GROUP;
+        constexpr int PIECES = 128 * (PANEL / 4) / 512;
+        uint4 v[PIECES];
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            const int piece = threadIdx.x + 512 * i, row = piece / (PANEL / 4), at = b0 + 16 * (piece % (PANEL / 4));
+            const uint8_t *src = p.S + (n0 + row < p.N ? n0 + row : p.N - 1) * p.lds + at;
+            uint32_t e[4] = {0, 0, 0, 0};
+            if (at + 16 <= row_bytes) {
+                __builtin_memcpy(e, src, 16);
+            } else if (at < row_bytes) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    if (at + 4 * k + 4 <= row_bytes) {
+                        __builtin_memcpy(&e[k], src + 4 * k, 4);
+                    } else {
+#pragma unroll
+                        for (int x = 0; x < 3; ++x)
+                            if (at + 4 * k + x < row_bytes) e[k] |= (uint32_t)src[4 * k + x] << (8 * x);
+                    }
+                }
+            }
+            v[i] = make_uint4(e[0], e[1], e[2], e[3]);
+        }
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            const int piece = threadIdx.x + 512 * i;
+            *reinterpret_cast<uint4 *>(scales + (piece / (PANEL / 4)) * PANEL + 4 * (piece % (PANEL / 4))) = v[i];
+        }
+    };
+    f32x4_t acc[NB][MBW];
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
-        for (int c = 0; c < MB; ++c) acc[b][c] = {0, 0, 0, 0};
+        for (int c = 0; c < MBW; ++c) acc[b][c] = {0, 0, 0, 0};
 
-    const int steps = (p.K + 127) / 128;
-    auto stage = [&](int t, int buf) {
-        const int chunks = (p.K - 128 * t) * (ROW / 128) / 16;  // of the last step, those behind K are not read: the first is, in their place, and not used
-#pragma unroll
-        for (int i = 0; i < DMAS; ++i) {
-            uint32_t c = ((uint32_t)(lane % CH)) ^ (uint32_t)(((nw * DMAS + i) * ROWS_PER + lane / CH) % CH);
-            c = (int)c < chunks ? c : 0;
-            lvx_dma16(a_base, a_off[i] + (uint32_t)t * ROW + 16 * c, lds0 + buf * STAGE + i * 1024);
-        }
-    };
-    auto fetch = [&](int t, uint4 (&w)[NB]) {
-        const bool in = 128 * t + 32 * g < p.K;
+    struct operands_t {
+        uint4 a[MBW][AV], w[NB];
+        uint32_t s[NB];
+    } x[2];
+    auto read = [&](int j, operands_t &d) {
+        const int t = step(j);
+        if (t >= steps) return;
+        const char *a_src = lds + kg * RING * A_STAGE + (j % RING) * A_STAGE + (mw * 16 * MBW + r) * ROW;
+        const char *w_src = lds + 2 * RING * A_STAGE + (kg * 2 + ((j >> 1) & 1)) * W_STAGE + (nw * 64 + r) * 128;
+        const uint8_t *mine = reinterpret_cast<const uint8_t *>(scales + (nw * 64 + r) * PANEL + t % PANEL) + g;
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
-            w[b] = make_uint4(0, 0, 0, 0);
-            if (in) w[b] = *reinterpret_cast<const uint4 *>(w_row[b] + (size_t)64 * t);
+            d.w[b] = *reinterpret_cast<const uint4 *>(w_src + b * 16 * 128 + 16 * ((4 * (j & 1) + g) ^ (r % 8)));
+            d.s[b] = (uint32_t)mine[16 * b * PANEL * 4] << (MODE == A_NATIVE ? 0 : 23);
+        }
+#pragma unroll
+        for (int c = 0; c < MBW; ++c)
+#pragma unroll
+            for (int i = 0; i < AV; ++i) {
+                const int chunk = MODE == A_BF16 ? 4 * g + i : MODE == A_WIDEN ? 2 * g + i : g + 4 * i;
+                d.a[c][i] = *reinterpret_cast<const uint4 *>(a_src + c * 16 * ROW + 16 * (chunk ^ (r % CH)));
+            }
+        const int left = p.K - 128 * t;
+        if (left < 128) {  // lanes of channels behind K multiply zeros
+#pragma unroll
+            for (int c = 0; c < MBW; ++c)
+#pragma unroll
+                for (int i = 0; i < AV; ++i)
+                    if ((MODE == A_NATIVE ? 16 * g + 64 * i : 32 * g) >= left) d.a[c][i] = make_uint4(0, 0, 0, 0);
+#pragma unroll
+            for (int b = 0; b < NB; ++b) d.s[b] = 32 * g < left ? d.s[b] : 127u << (MODE == A_NATIVE ? 0 : 23);
         }
     };
-    // A group takes every fourth pair of steps: a pair is a whole line of a weight row.
-    const int pairs = (steps + 1) / 2, rounds = (pairs + KG - 1) / KG;
-    uint4 w[2][2][NB];
-    auto fetch_pair = [&](int q, uint4 (&d)[2][NB]) {
-        if (2 * q < steps) fetch(2 * q, d[0]);
-        if (2 * q + 1 < steps) fetch(2 * q + 1, d[1]);
-    };
-    if (2 * kg < steps) stage(2 * kg, 0), fetch_pair(kg, w[0]);
-    auto step = [&](int t, int next, int buf, uint4 (&wi)[NB]) {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    // Iteration j multiplies step j (in registers), reads step j + 1 (in LDS) and requests the rows of step j + RING into the place of step j, and the weights of the pair that
+    // begins with it into the place of the pair before, which every wave has read.  Requests complete in order: with three stages those of this iteration may be left when
+    // the ones before have to be there.
+    auto iteration = [&](int j, bool odd, const operands_t &now, operands_t &next) {
         __syncthreads();
-        if (next < steps) stage(next, buf ^ 1);
-        if (t < steps) {
-            const char *src = lds + (kg * 2 + buf) * STAGE + r * ROW;
-            const uint8_t *mine = reinterpret_cast<const uint8_t *>(scales + (nw * 64 + r) * (PANEL + 1) + t % PANEL) + g;
-            uint4 a[MB][AV];
-            const int left = p.K - 128 * t;
-#pragma unroll
-            for (int c = 0; c < MB; ++c)
-#pragma unroll
-                for (int j = 0; j < AV; ++j) {
-                    const int chunk = MODE == A_BF16 ? 4 * g + j : MODE == A_WIDEN ? 2 * g + j : g + 4 * j;
-                    a[c][j] = *reinterpret_cast<const uint4 *>(src + c * 16 * ROW + 16 * (chunk ^ (r % CH)));
-                }
-            uint32_t sc[NB];
-#pragma unroll
-            for (int b = 0; b < NB; ++b) sc[b] = (uint32_t)mine[16 * b * (PANEL + 1) * 4] << (MODE == A_NATIVE ? 0 : 23);
-            if (left < 128) {
-#pragma unroll
-                for (int c = 0; c < MB; ++c)
-#pragma unroll
-                    for (int j = 0; j < AV; ++j)
-                        if ((MODE == A_NATIVE ? 16 * g + 64 * j : 32 * g) >= left) a[c][j] = make_uint4(0, 0, 0, 0);
-#pragma unroll
-                for (int b = 0; b < NB; ++b) sc[b] = 32 * g < left ? sc[b] : 127u << (MODE == A_NATIVE ? 0 : 23);
-            }
-            fp4_multiply<MODE, MB, NB>(acc, wi, sc, a);
+        const bool more = step(j + RING) < steps, more_w = more && odd == (RING == 3);
+        if (more) stage_a(j + RING);
+        if (more_w) stage_w(j + RING);
+        if (odd && (j + 1) % (PANEL / 2) == 0) {
+            load_scales(j + 1);
+            __syncthreads();
         }
+        read(j + 1, next);
+        if (step(j) < steps) fp4_multiply<MODE, MBW, NB>(acc, now.w, now.s, now.a);
+        if (RING == 3 && more_w)
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(DA + DW) : "memory");
+        else if (RING == 3 && more)
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(DA) : "memory");
+        else
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     };
-    auto round = [&](int i, uint4 (&wi)[2][NB], uint4 (&wn)[2][NB]) {
-        const int q = kg + KG * i;
-        if (i % (PANEL / 2 / KG) == 0) {
-            // the next 64 steps' scales, 16 bytes = 4 steps of a column a piece
-            if (i > 0) __syncthreads();
-            const int b0 = 2 * KG * 4 * i, row_bytes = p.K / 32;
-            uint4 v[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int piece = threadIdx.x + 512 * j, row = piece >> 4, at = b0 + 16 * (piece & 15);
-                const int n = blockIdx.x * 128 + row < p.N ? blockIdx.x * 128 + row : p.N - 1;
-                const uint8_t *src = p.S + n * p.lds + at;
-                v[j] = make_uint4(0, 0, 0, 0);
-                if (at + 16 <= row_bytes) {
-                    __builtin_memcpy(&v[j], src, 16);
-                } else if (at < row_bytes) {
-                    uint32_t e[4] = {0, 0, 0, 0};
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        if (at + 4 * k + 4 <= row_bytes) {
-                            __builtin_memcpy(&e[k], src + 4 * k, 4);
-                        } else {
-#pragma unroll
-                            for (int x = 0; x < 3; ++x)
-                                if (at + 4 * k + x < row_bytes) e[k] |= (uint32_t)src[4 * k + x] << (8 * x);
-                        }
-                    }
-                    v[j] = make_uint4(e[0], e[1], e[2], e[3]);
-                }
-            }
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int piece = threadIdx.x + 512 * j;
-                uint32_t *dst = scales + (piece >> 4) * (PANEL + 1) + 4 * (piece & 15);
-                dst[0] = v[j].x, dst[1] = v[j].y, dst[2] = v[j].z, dst[3] = v[j].w;
-            }
-        }
-        step(2 * q, 2 * q + 1, 0, wi[0]);
-        if (2 * (q + KG) < steps) fetch_pair(q + KG, wn);
-        step(2 * q + 1, 2 * (q + KG), 1, wi[1]);
-    };
-    for (int i = 0; i < rounds; i += 2) {
-        round(i, w[0], w[1]);
-        if (i + 1 < rounds) round(i + 1, w[1], w[0]);
+    for (int j = 0; j < RING; ++j)
+        if (step(j) < steps) stage_a(j);
+    if (step(0) < steps) stage_w(0);
+    if (RING == 3 && step(2) < steps) stage_w(2);
+    load_scales(0);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    read(0, x[0]);
+    for (int j = 0; j < 2 * rounds; j += 2) {
+        iteration(j, false, x[0], x[1]);
+        iteration(j + 1, true, x[1], x[0]);
     }
     __syncthreads();
 
-    float row_scale[MB];
-    fp4_row_scales<MODE, MB>(p, m0 + r, row_scale);
-    // the groups' sums: 2 and 3 to 0 and 1, then 1 to 0
+    float row_scale[MBW];
+    fp4_row_scales<MODE, MBW>(p, m0 + mw * 16 * MBW + r, row_scale);
+    // each group finishes half of the columns' blocks with the other's sums
     f32x4_t *part = reinterpret_cast<f32x4_t *>(lds);
 #pragma unroll
-    for (int half = 2; half >= 1; half >>= 1) {
-        if (kg >= half && kg < 2 * half) {
+    for (int b = 0; b < NB / 2; ++b)
 #pragma unroll
-            for (int b = 0; b < NB; ++b)
+        for (int c = 0; c < MBW; ++c) part[((wave * (NB / 2) + b) * MBW + c) * 64 + lane] = kg == 0 ? acc[b + NB / 2][c] : acc[b][c];
+    __syncthreads();
 #pragma unroll
-                for (int c = 0; c < MB; ++c) part[(((kg - half) * 2 + nw) * NB * MB + b * MB + c) * 64 + lane] = acc[b][c];
+    for (int b = 0; b < NB / 2; ++b) {
+        f32x4_t sum[MBW];
+#pragma unroll
+        for (int c = 0; c < MBW; ++c) {
+            const f32x4_t its = part[(((wave ^ 4) * (NB / 2) + b) * MBW + c) * 64 + lane];
+            sum[c] = kg == 0 ? acc[b][c] + its : its + acc[b + NB / 2][c];  // group 0's sum first
         }
-        __syncthreads();
-        if (kg < half) {
-#pragma unroll
-            for (int b = 0; b < NB; ++b)
-#pragma unroll
-                for (int c = 0; c < MB; ++c) acc[b][c] += part[((kg * 2 + nw) * NB * MB + b * MB + c) * 64 + lane];
-        }
-        __syncthreads();
+        fp4_store<MBW>(p, m0 + mw * 16 * MBW + r, n0 + nw * 64 + 16 * (b + (kg == 0 ? 0 : NB / 2)) + 4 * g, sum, row_scale);
     }
-    if (kg > 0) return;
-#pragma unroll
-    for (int b = 0; b < NB; ++b) fp4_store<MB>(p, m0 + r, n0 + 16 * b + 4 * g, acc[b], row_scale);
 }
 
 // 32 channels of a row per thread
@@ -452,11 +466,13 @@ void launch_few(const fp4_args_t &p, int most_waves, hipStream_t stream) {
     hipLaunchKernelGGL((lvx_fp4_few_kernel<MODE, MB, NB, U>), grid, dim3(64 * waves), (waves - 1) * NB * MB * 1024, stream, p);
 }
 
-template <int MODE, int MB>
+template <int MODE, int MBW, int RING>
 void launch_tile(const fp4_args_t &p, hipStream_t stream) {
-    const dim3 grid((p.N + 127) / 128, (p.M + 16 * MB - 1) / (16 * MB));
-    const int stages = 4 * 2 * MB * 16 * (MODE == A_BF16 ? 256 : 128), sums = 2 * 2 * 4 * MB * 1024;
-    hipLaunchKernelGGL((lvx_fp4_tile_kernel<MODE, MB>), grid, dim3(512), stages > sums ? stages : sums, stream, p);
+    constexpr int stages = 2 * RING * 32 * MBW * (MODE == A_BF16 ? 256 : 128) + 4 * 128 * 128, sums = 8 * 2 * MBW * 1024;
+    constexpr int bytes = stages + 128 * PANEL * 4;
+    static_assert(bytes <= 160 * 1024 && sums <= bytes, "LDS");
+    const dim3 grid((p.N + 127) / 128, (p.M + 32 * MBW - 1) / (32 * MBW));
+    hipLaunchKernelGGL((lvx_fp4_tile_kernel<MODE, MBW, RING>), grid, dim3(512), bytes, stream, p);
 }
 
 // Few rows.  More columns to a workgroup share the loads of A; that pays where enough workgroups are left (5120 columns, 5120 channels, 4 rows: 8.2 us with two blocks of
@@ -475,40 +491,40 @@ void linear_few(const fp4_args_t &p, hipStream_t stream) {
         two ? launch_few<MODE, 4, 2, MODE == A_BF16 ? 1 : 2>(p, 4, stream) : launch_few<MODE, 4, 1, MODE == A_BF16 ? 1 : 2>(p, 4, stream);
 }
 
-// Rows of a tile, in blocks of 16: the fewest rounds of the chip, weighed with what a round costs.  A step takes about as long as 8 blocks of 8-bit rows (4 of bf16) even
-// without any (its loads' way); measured at 5120 channels, one round: 22, 26 and 31 us with 2, 4 and 6 blocks of 8-bit rows.
-int tile_blocks(const fp4_args_t &p, const int *choices, int n, int cost_of_block) {
+// Rows of a tile, in blocks of 32: the fewest rounds of the chip, weighed with what a round costs.  A step takes about as long as two blocks even without any (its requests, its
+// weights, its barrier); 5120 channels, one round: 15, 19 and 22 us with 1, 2 and 3 blocks of 8-bit rows, 23 and 29 with 1 and 2 of bf16.
+int tile_blocks(const fp4_args_t &p, int most) {
     int best = 0;
     int64_t least = INT64_MAX;
-    for (int i = 0; i < n; ++i) {
-        const int64_t groups = (int64_t)((p.N + 127) / 128) * ((p.M + 16 * choices[i] - 1) / (16 * choices[i]));
-        const int64_t cost = (groups + LVX_NUM_CU - 1) / LVX_NUM_CU * (8 + cost_of_block * choices[i]);
-        if (cost < least) least = cost, best = choices[i];
+    for (int mbw = most; mbw >= 1; --mbw) {
+        const int64_t groups = (int64_t)((p.N + 127) / 128) * ((p.M + 32 * mbw - 1) / (32 * mbw));
+        const int64_t cost = (groups + LVX_NUM_CU - 1) / LVX_NUM_CU * (2 + mbw);
+        if (cost < least) least = cost, best = mbw;
     }
     return best;
 }
 
 void linear_launch(const fp4_args_t &p, bool a8, hipStream_t stream) {
-    // Tiles from the product of rows (in blocks) and columns on where they fill the chip and are faster (bf16: 96 x 5120 x 1280 10.7 us against 12.8, 96 x 1280 x 1280 10.4
-    // against 8.3; 8-bit rows: 96 x 13824 x 5120 29 against 47, 48 x 13824 x 1280 13.7 against 9.5), and rows within reach of the tiles' 32-bit offsets.
+    // The mixed instruction lines the products of four neighbouring channels up with the largest of them and cuts what lies 12 binary places below its leading bit (measured;
+    // the fours and the steps are added in fp32).  An output in bf16 is rounded at 8 places anyway, and on normal rows the cut is 4e-6 of a sum: it is taken there, for
+    // twice the rate.  Outputs in fp32 get the rows widened to bf16, whose products and sums are fp32's.
+    const bool native = a8 && p.epi != LVX_EPI_RESID_GATE_F32 && p.epi != LVX_EPI_STORE_F32;
+    // Tiles from the product of rows (in blocks of 16) and columns on where they are faster: 96 x 5120 x 5120 15, 22 and 23 us (mixed, widened, bf16) against 24, 24 and 37 of
+    // the few-row kernel, 200 x 1280 x 5120 15, 22 and 23 against 18, 18 and 28, 48 x 5120 x 5120 15, 22 and 23 against 16, 16 and 20.  Rows have to be within reach of their
+    // 32-bit offsets.
     const int64_t area = (int64_t)((p.M + 15) / 16) * p.N;
-    const bool tiles = p.M > 32 && area >= (a8 ? 50000 : 24000) && p.lda < (1 << 24);
+    const bool tiles = p.M > 32 && area >= (a8 && !native ? 30000 : 16000) && p.lda < (1 << 24) && p.ldw < (1 << 24);
     if (!tiles) {
         a8 ? linear_few<A_WIDEN>(p, stream) : linear_few<A_BF16>(p, stream);
-    } else if (!a8) {
-        static const int choices[] = {3, 2, 1};
-        const int mb = tile_blocks(p, choices, 3, 2);
-        mb == 3 ? launch_tile<A_BF16, 3>(p, stream) : mb == 2 ? launch_tile<A_BF16, 2>(p, stream) : launch_tile<A_BF16, 1>(p, stream);
-    } else if (p.epi == LVX_EPI_RESID_GATE_F32 || p.epi == LVX_EPI_STORE_F32) {
-        // The mixed instruction aligns the 128 products of a step before it adds them and drops what lies about 2^-17 below the largest: nothing beside a bf16 output's rounding,
-        // but more than fp32 sums lose.  Outputs in fp32 get the rows widened to bf16.
-        static const int choices[] = {4, 2};
-        tile_blocks(p, choices, 2, 2) == 4 ? launch_tile<A_WIDEN, 4>(p, stream) : launch_tile<A_WIDEN, 2>(p, stream);
-    } else {
-        static const int choices[] = {6, 4, 2};
-        const int mb = tile_blocks(p, choices, 3, 1);
-        mb == 6 ? launch_tile<A_NATIVE, 6>(p, stream) : mb == 4 ? launch_tile<A_NATIVE, 4>(p, stream) : launch_tile<A_NATIVE, 2>(p, stream);
+        return;
     }
+    const int mbw = tile_blocks(p, a8 ? 3 : 2);
+    if (!a8)
+        mbw == 2 ? launch_tile<A_BF16, 2, 2>(p, stream) : launch_tile<A_BF16, 1, 3>(p, stream);
+    else if (native)
+        mbw == 3 ? launch_tile<A_NATIVE, 3, 3>(p, stream) : mbw == 2 ? launch_tile<A_NATIVE, 2, 3>(p, stream) : launch_tile<A_NATIVE, 1, 3>(p, stream);
+    else
+        mbw == 3 ? launch_tile<A_WIDEN, 3, 3>(p, stream) : mbw == 2 ? launch_tile<A_WIDEN, 2, 3>(p, stream) : launch_tile<A_WIDEN, 1, 3>(p, stream);
 }
 
 lvx_status_t linear(const void *a, int64_t lda, const float *row_scales, bool a8, const void *w, int64_t ldw, const void *s, int64_t lds, void *c,
