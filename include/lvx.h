@@ -277,7 +277,7 @@ lvx_status_t lvx_layernorm_modulate(const void *dev_x, int64_t ldx, const float 
 /* h = x + resid;  y = h / sqrt(mean_c(h^2) + eps) * gain,  fp32 throughout; the norm sees h un-rounded.
  *   x bf16 or NULL (0); resid bf16, or fp32 with resid_is_f32 = 1 (strides in fp32 elements), or NULL (0), not both NULL; gain fp32 [d] or NULL (1).
  *   dev_sum (may be NULL; needs a residual): h in the residual's type.  dev_y: bf16.  Each output may be the buffer of an input of the same type
- *   and stride.  d % 8 == 0, d <= 16384, strides % 8 == 0.
+ *   and stride.  d % 8 == 0, d <= 16384, strides % 8 == 0, fewer than 2^22 tokens.
  * lvx_rmsnorm_residual_fp8: y leaves as E4M3 codes with one fp32 scale a row: scale = max|y| / 448 (1 for a zero row), code =
  *   E4M3(y * (448 / max|y|)), nearest-even: what lvx_linear_fp8_fp4 takes.  d % 16 == 0, ldq % 16 == 0.  A row that holds a NaN or an
  *   infinity has a NaN scale. */
@@ -289,13 +289,14 @@ lvx_status_t lvx_rmsnorm_residual_fp8(const void *dev_x, int64_t ldx, const void
                                       float *dev_row_scales, lvx_stream_t stream);
 
 /* bf16 [rows][ld] -> E2M1 codes [rows][ldq bytes], two to a byte with the even column in the low half, and one E8M0 byte (2^(byte - 127)) per 32
- * columns, [rows][lds bytes]: the smallest exponent >= -120 with max|x| <= 7 * 2^e; nearest, ties to the even code, saturating at 6.  A group that holds
- * a NaN or an infinity gets scale 255 (NaN).  cols % 32 == 0, ldq >= cols / 2 and % 16 == 0, lds >= cols / 32.  For weights, once. */
+ * columns, [rows][lds bytes]: the smallest exponent >= -120 with max|x| <= 7 * 2^e; nearest, ties to the even code, saturating at 6 (products of 2^128 are infinite in
+ * bf16: elements above 1.75 * 2^127).  A group that holds a NaN or an infinity gets scale 255 (NaN).  cols % 32 == 0, ldq >= cols / 2 and % 16 == 0, lds >= cols / 32.  For weights, once. */
 lvx_status_t lvx_fp4_quantize(const void *dev_x, int64_t ld, int32_t rows, int32_t cols, void *dev_q, int64_t ldq, void *dev_scales, int64_t lds,
                               lvx_stream_t stream);
 /* C[M][N] = epilogue(A[M][K] * W[N][K]^T), W in that form (any scale byte; 255 is NaN), fp32 accumulate; for one row as for a prompt.
- *   lvx_linear_fp4: A bf16, lda % 8 == 0.   lvx_linear_fp8_fp4: A E4M3 codes with a scale per row, lda in bytes % 16 == 0.
- * K % 32 == 0, N % 8 == 0, ldc, ldr % 8 == 0, ldw in bytes % 16 == 0.  Epilogues STORE, GELU_TANH, RESID_GATE, RESID_GATE_F32, STORE_F32; C may alias R.
+ *   lvx_linear_fp4: A bf16, lda % 8 == 0.   lvx_linear_fp8_fp4: A E4M3 codes with a scale per row, lda in bytes % 16 == 0.  Many of those rows with bf16 outputs are
+ *   multiplied 8 by 4 bits, where products of four neighbouring channels are lined up with the largest of them and cut 12 binary places below its leading bit.
+ * K % 32 == 0, N % 8 == 0, N <= 2^24, M <= 2^20, ldc, ldr % 8 == 0, ldw in bytes % 16 == 0.  Epilogues STORE, GELU_TANH, RESID_GATE, RESID_GATE_F32, STORE_F32; C may alias R.
  * The same call gives the same bits; the order of summation depends on M, N and K. */
 lvx_status_t lvx_linear_fp4(const void *dev_a, int64_t lda, const void *dev_wq, int64_t ldw, const void *dev_w_scales, int64_t lds, void *dev_c,
                             int64_t ldc, int32_t M, int32_t N, int32_t K, lvx_epilogue_t epi, const void *dev_resid, int64_t ldr,

@@ -536,10 +536,10 @@ lvx_status_t linear(const void *a, int64_t lda, const float *row_scales, bool a8
                 LVX_ERR_INVALID_ARG, "pointers must be 16-byte aligned (scales and gate as their type)");
     LVX_REQUIRE(M >= 0 && N > 0 && K > 0, LVX_ERR_SHAPE, "M %d, N %d, K %d", M, N, K);
     LVX_REQUIRE(K % LVX_FP4_GROUP == 0, LVX_ERR_SHAPE, "K %d must be a multiple of %d", K, LVX_FP4_GROUP);
-    LVX_REQUIRE(N % 8 == 0, LVX_ERR_SHAPE, "N %d must be a multiple of 8", N);
+    LVX_REQUIRE(N % 8 == 0 && N <= 1 << 24, LVX_ERR_SHAPE, "N %d must be a multiple of 8, at most 2^24", N);
     LVX_REQUIRE(lda >= K && lda % (a8 ? 16 : 8) == 0 && ldw >= K / 2 && ldw % 16 == 0 && lds >= K / LVX_FP4_GROUP && ldc >= N && ldc % 8 == 0,
                 LVX_ERR_SHAPE, "bad leading dimension");
-    LVX_REQUIRE(M <= 65535 * 16, LVX_ERR_SHAPE, "M %d is more than %d rows", M, 65535 * 16);
+    LVX_REQUIRE(M <= 1 << 20, LVX_ERR_SHAPE, "M %d is more than 2^20 rows", M);
     LVX_REQUIRE(epi == LVX_EPI_STORE || epi == LVX_EPI_GELU_TANH || epi == LVX_EPI_RESID_GATE || epi == LVX_EPI_RESID_GATE_F32 || epi == LVX_EPI_STORE_F32,
                 LVX_ERR_INVALID_ARG, "unknown epilogue %d", (int)epi);
     if (epi == LVX_EPI_RESID_GATE || epi == LVX_EPI_RESID_GATE_F32) {

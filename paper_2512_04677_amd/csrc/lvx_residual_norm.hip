@@ -10,6 +10,7 @@
 namespace {
 
 constexpr float E4M3_MAX = 448.0f;
+constexpr int MAX_TOKENS = 1 << 22;  // a launch holds fewer than 2^32 threads, and a long row takes 1024
 
 struct norm_args_t {
     const bf16_t *x;     // may be NULL
@@ -59,7 +60,7 @@ __global__ void __launch_bounds__(T < 256 ? 256 : T) lvx_rmsnorm_residual_kernel
     __shared__ float lds_sum[16];
     __shared__ uint32_t lds_max[16];
     const int t = threadIdx.x % T;
-    const int row = blockIdx.x * ROWS + threadIdx.x / T;
+    const int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / T;
     if (row >= p.n_tokens) return;  // whole waves, and no barrier where ROWS > 1
 
     float h[NI][8];
@@ -170,7 +171,7 @@ lvx_status_t entry(const void *x, int64_t ldx, const void *r, int64_t ldr, int32
     LVX_REQUIRE(eps >= 0.f, LVX_ERR_INVALID_ARG, "eps must not be negative");
     const int step = fp8 ? 16 : 8;
     LVX_REQUIRE(d > 0 && d % step == 0 && d <= 16384, LVX_ERR_SHAPE, "d %d must be a positive multiple of %d, at most 16384", d, step);
-    LVX_REQUIRE(n >= 0, LVX_ERR_SHAPE, "n_tokens %d is negative", n);
+    LVX_REQUIRE(n >= 0 && n < MAX_TOKENS, LVX_ERR_SHAPE, "n_tokens %d is negative or not below %d", n, MAX_TOKENS);
     LVX_REQUIRE((x == nullptr || (ldx >= d && ldx % 8 == 0)) && (r == nullptr || (ldr >= d && ldr % 8 == 0)) &&
                     (sum == nullptr || (ld_sum >= d && ld_sum % 8 == 0)) && ldy >= d && ldy % step == 0,
                 LVX_ERR_SHAPE, "row strides must be >= d and multiples of 8 (16 for the 8-bit rows)");

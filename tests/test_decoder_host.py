@@ -28,7 +28,7 @@ def test_norm_refusals():
     assert status(x=ODD) == 1 and status(r=ODD) == 1 and status(g=ODD) == 1 and status(s=ODD) == 1 and status(y=ODD) == 1
     assert status(f32=2) == 1 and status(eps=-1.0) == 1 and status(eps=float("nan")) == 1
     assert status(d=60) == 2 and status(d=0) == 2 and status(d=16392, ldx=1 << 15, ldr=1 << 15, lds=1 << 15, ldy=1 << 15) == 2
-    assert status(n=-1) == 2 and status(ldx=56) == 2 and status(ldr=68) == 2 and status(lds=56) == 2 and status(ldy=56) == 2
+    assert status(n=-1) == 2 and status(n=1 << 22) == 2 and status(ldx=56) == 2 and status(ldr=68) == 2 and status(lds=56) == 2 and status(ldy=56) == 2
     assert status(r=None, s=None, ldr=0, lds=0) == 0
     g = lvx.load().lvx_rmsnorm_residual_fp8
     assert g(P, 72, P, 72, 0, P, 1e-6, 0, 72, P, 72, P, 80, P, None) == 2          # d % 16
@@ -55,7 +55,7 @@ def test_quantize_and_linear_refusals():
     assert status(ldw=16) == 2 and status(ldw=40) == 2 and status(lds=1) == 2 and status(ldc=8) == 2 and status(ldc=20) == 2
     assert status(epi=4) == 1 and status(epi=5) == 1 and status(epi=7) == 1 and status(epi=2) == 1 and status(epi=3) == 1
     assert status(epi=2, r=P, ldr=8) == 2 and status(epi=2, r=P, ldr=16) == 0 and status(epi=2, r=ODD, ldr=16) == 1
-    assert status(gate=C.c_void_p(4097)) == 1 and status(M=65535 * 16 + 1) == 2
+    assert status(gate=C.c_void_p(4097)) == 1 and status(M=(1 << 20) + 1) == 2 and status(N=(1 << 24) + 8, ldc=1 << 25) == 2
 
     def status8(sa=P, **kw):
         v = list({**ok, **kw}.values())

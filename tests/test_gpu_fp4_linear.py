@@ -177,3 +177,27 @@ def test_mixed_products_lose_no_more_than_that(lvx):
     err = np.abs(S.to_f64(out) - ref) - 2.0 ** -8 * np.abs(ref)
     print("beyond the output's rounding: %.3f of the bound at most" % (err / cut).max(), flush=True)
     assert np.all(err <= cut + off) and np.all(np.abs(S.to_f64(o32) - ref) <= off)
+
+
+@pytest.mark.parametrize("a8,f32", [(False, False), (True, False), (True, True)])
+def test_non_finite_weights_and_rows_of_tiles(lvx, a8, f32):
+    """A NaN scale makes NaN of its column, a NaN in a row of its row, whatever lies behind K in a padded row of nothing."""
+    M, N, K, pad = 48, 5464, 288, 32
+    q, s = lvx.lvx_fp4_quantize(S.randn_bf16((N, K), S.seed_of("nft", "w"), 1.0, device=DEV))
+    s = s.clone()
+    s[7, 8], s[5000, 0] = 255, 255
+    out = torch.empty(M, N, dtype=torch.float32 if f32 else torch.bfloat16, device=DEV)
+    if a8:
+        a = torch.full((M, K + pad), 0x7f, dtype=torch.uint8, device=DEV)
+        a[:, :K] = S.randn_f32((M, K), S.seed_of("nft", "a"), 60.0, device=DEV).to(torch.float8_e4m3fn).view(torch.uint8)
+        a[33, 280] = 0x7f
+        lvx.lvx_linear_fp8_fp4(a[:, :K], torch.ones(M, device=DEV), q, s, out, lvx.EPI_STORE_F32 if f32 else lvx.EPI_STORE)
+    else:
+        a = torch.full((M, K + pad), float("nan"), dtype=torch.bfloat16, device=DEV)
+        a[:, :K] = S.randn_bf16((M, K), S.seed_of("nft", "a"), 1.0, device=DEV)
+        a[33, 280] = float("nan")
+        lvx.lvx_linear_fp4(a[:, :K], q, s, out)
+    bad = torch.zeros(M, N, dtype=torch.bool, device=DEV)
+    bad[:, 7] = bad[:, 5000] = True
+    bad[33] = True
+    assert torch.equal(torch.isnan(out), bad)
