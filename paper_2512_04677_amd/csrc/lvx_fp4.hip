@@ -254,6 +254,106 @@ __global__ void __launch_bounds__(512) lvx_fp4_few_kernel(fp4_args_t p) {
     }
 }
 
+// ---- rows that fit the LDS ----------------------------------------------------------------------------------------------
+// The same for up to sixteen rows that lie in LDS whole (56 KB of them), with the columns' scales beside them, brought there once while the first weights are on their
+// way: the loop then requests nothing but weights, two steps ahead of a wave's own.
+template <int MODE, int NB>
+__global__ void __launch_bounds__(512) lvx_fp4_resident_kernel(fp4_args_t p) {
+    constexpr int AV = MODE == A_BF16 ? 4 : 2, STEP_A = MODE == A_BF16 ? 256 : 128;
+    extern __shared__ char lds[];  // rows, scales; then the partial sums
+    const int lane = threadIdx.x & 63, kw = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    const int r = lane & 15, g = lane >> 4;
+    const int n0 = blockIdx.x * 16 * NB;
+    const int row_bytes = p.K * (MODE == A_BF16 ? 2 : 1), a_pitch = row_bytes + 16, s_bytes = p.K / LVX_FP4_GROUP, s_pitch = ((s_bytes + 15) & ~15) + 4;
+    char *s_lds = lds + p.M * a_pitch;
+    const uint8_t *w_row[NB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+        const int n = n0 + 16 * b + r < p.N ? n0 + 16 * b + r : p.N - 1;  // columns past the end repeat the last one: they are read, multiplied and not stored
+        w_row[b] = p.W + n * p.ldw + 16 * g;
+    }
+    f32x4_t acc[NB][1];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) acc[b][0] = {0, 0, 0, 0};
+    const int whole = p.K / 128;
+    uint4 w[2][NB];
+    auto load = [&](int t, uint4 (&d)[NB]) {
+        if (t >= whole) return;
+#pragma unroll
+        for (int b = 0; b < NB; ++b) d[b] = *reinterpret_cast<const uint4 *>(w_row[b] + (size_t)64 * t);
+    };
+    load(kw, w[0]);
+    for (int m = 0; m < p.M; ++m)
+        for (int c = threadIdx.x; c < row_bytes / 16; c += blockDim.x)
+            *reinterpret_cast<uint4 *>(lds + m * a_pitch + 16 * c) = *reinterpret_cast<const uint4 *>(p.A + m * p.lda + 16 * c);
+    // scales: a thread takes 16 bytes of a column, a last piece byte by byte
+    for (int i = threadIdx.x; i < 16 * NB * 16; i += blockDim.x) {
+        const int row = i >> 4, n = n0 + row < p.N ? n0 + row : p.N - 1;
+        const uint8_t *src = p.S + n * p.lds;
+        for (int at = 16 * (i & 15); at < s_bytes; at += 256) {
+            uint32_t e[4] = {0, 0, 0, 0};
+            if (at + 16 <= s_bytes) {
+                __builtin_memcpy(e, src + at, 16);
+            } else {
+#pragma unroll
+                for (int x = 0; x < 15; ++x)
+                    if (at + x < s_bytes) e[x >> 2] |= (uint32_t)src[at + x] << (8 * (x & 3));
+            }
+            uint32_t *dst = reinterpret_cast<uint32_t *>(s_lds + row * s_pitch + at);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) dst[x] = e[x];
+        }
+    }
+    __syncthreads();
+    load(kw + waves, w[1]);
+    const char *a_row = lds + (r < p.M ? r : p.M - 1) * a_pitch;
+    const uint8_t *s_row = reinterpret_cast<const uint8_t *>(s_lds + r * s_pitch) + g;
+    auto step = [&](int t, bool in, const uint4 (&wt)[NB]) {
+        uint4 a[1][AV];
+        uint32_t sc[NB];
+#pragma unroll
+        for (int j = 0; j < AV; ++j) {
+            a[0][j] = make_uint4(0, 0, 0, 0);
+            if (in) a[0][j] = *reinterpret_cast<const uint4 *>(a_row + STEP_A * t + (STEP_A / 4) * g + 16 * j);
+        }
+#pragma unroll
+        for (int b = 0; b < NB; ++b) sc[b] = in ? (uint32_t)s_row[16 * b * s_pitch + 4 * t] << 23 : 127u << 23;
+        fp4_multiply<MODE, 1, NB>(acc, wt, sc, a);
+    };
+    for (int t = kw; t < whole; t += 2 * waves) {
+        step(t, true, w[0]);
+        load(t + 2 * waves, w[0]);
+        if (t + waves < whole) {
+            step(t + waves, true, w[1]);
+            load(t + 3 * waves, w[1]);
+        }
+    }
+    // a last step of one to three groups of 32 channels: the other lanes multiply zeros
+    if (p.K % 128 != 0 && kw == whole % waves) {
+        const bool in = 128 * whole + 32 * g < p.K;
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            w[0][b] = make_uint4(0, 0, 0, 0);
+            if (in) w[0][b] = *reinterpret_cast<const uint4 *>(w_row[b] + (size_t)64 * whole);
+        }
+        step(whole, in, w[0]);
+    }
+
+    float row_scale[1];
+    fp4_row_scales<MODE, 1>(p, r, row_scale);
+    __syncthreads();
+    f32x4_t *part = reinterpret_cast<f32x4_t *>(lds);  // [waves][NB][64]
+#pragma unroll
+    for (int b = 0; b < NB; ++b) part[(kw * NB + b) * 64 + lane] = acc[b][0];
+    __syncthreads();
+    // a wave finishes every waves-th block of columns, adding in the order of the waves
+    for (int b = kw; b < NB; b += waves) {
+        f32x4_t v[1] = {part[b * 64 + lane]};
+        for (int k = 1; k < waves; ++k) v[0] += part[(k * NB + b) * 64 + lane];
+        fp4_store<1>(p, r, n0 + 16 * b + 4 * g, v, row_scale);
+    }
+}
+
 // ---- many rows: tiles of 32 MBW rows and 128 columns ---------------------------------------------------------------------
 // Bound by the matrix cores and the LDS.  Eight waves: two groups over K, every second pair of steps each, of two by two waves (half the rows, half the columns).  Rows
 // and weights come by direct loads to LDS, RING steps and a pair or two of steps ahead: a stage of the weights is a pair, because a weight row's 128 channels are half a
@@ -466,6 +566,13 @@ void launch_few(const fp4_args_t &p, int most_waves, hipStream_t stream) {
     hipLaunchKernelGGL((lvx_fp4_few_kernel<MODE, MB, NB, U>), grid, dim3(64 * waves), (waves - 1) * NB * MB * 1024, stream, p);
 }
 
+template <int MODE, int NB>
+void launch_resident(const fp4_args_t &p, hipStream_t stream) {
+    const int steps = (p.K + 127) / 128, rounds = (steps + 7) / 8, waves = (steps + rounds - 1) / rounds;
+    const int operands = p.M * (p.K * (MODE == A_BF16 ? 2 : 1) + 16) + 16 * NB * (((p.K / LVX_FP4_GROUP + 15) & ~15) + 4), sums = waves * NB * 1024;
+    hipLaunchKernelGGL((lvx_fp4_resident_kernel<MODE, NB>), dim3((p.N + 16 * NB - 1) / (16 * NB)), dim3(64 * waves), operands > sums ? operands : sums, stream, p);
+}
+
 template <int MODE, int MBW, int RING>
 void launch_tile(const fp4_args_t &p, hipStream_t stream) {
     constexpr int stages = 2 * RING * 32 * MBW * (MODE == A_BF16 ? 256 : 128) + 4 * 128 * 128, sums = 8 * 2 * MBW * 1024;
@@ -479,6 +586,12 @@ void launch_tile(const fp4_args_t &p, hipStream_t stream) {
 // columns, 8.9 with one; 13824 columns, 16 rows in bf16: 14.3 with four, 17.5 with two; 1280 columns: one is fastest).
 template <int MODE>
 void linear_few(const fp4_args_t &p, hipStream_t stream) {
+    // Rows that fit the LDS beside others' (two workgroups a unit at least) and are long enough to pay for the way there: one row x 15360 x 5120 9.5 us against 12.0, 4 rows 10.9 against
+    // 13.1, 4 8-bit rows x 5120 x 13824 12.4 against 13.8; but 8 bf16 rows of 5120 (82 KB) 10.2 against 8.9, one row x 1280 x 1280 3.9 against 3.2.
+    if (p.M <= 16 && p.K >= 4096 && (int64_t)p.M * p.K * (MODE == A_BF16 ? 2 : 1) <= 56 * 1024) {
+        p.N >= 8192 ? launch_resident<MODE, 2>(p, stream) : launch_resident<MODE, 1>(p, stream);
+        return;
+    }
     const int blocks = (p.M + 15) / 16, tiles = (blocks + 3) / 4, mb = (blocks + tiles - 1) / tiles;
     const bool two = p.N >= 4096;
     if (mb == 1)

@@ -101,10 +101,12 @@ SHAPES = [(1, 8, 32), (1, 264, 5120), (2, 40, 96), (15, 72, 160), (16, 520, 1184
 
 # and products that fill the chip: every height of a tile, one step and many, odd numbers of steps and of pairs, a step that is not whole, scales of more than 48 steps
 TILES = [(40, 5464, 32), (35, 6000, 416), (70, 4104, 6304), (545, 2568, 96), (550, 5000, 544), (544, 2560, 160), (33, 13824, 768), (97, 5128, 1024)]
+# few rows of many channels, which lie in LDS whole: one and several blocks of columns, steps that the waves share unevenly, a step that is not whole
+LONG = [(1, 8, 4096), (1, 8200, 5120), (3, 40, 4128), (2, 8232, 6304), (7, 136, 4000), (13, 264, 4096), (4, 72, 13824)]
 
 
 @pytest.mark.parametrize("a8", [False, True])
-@pytest.mark.parametrize("M,N,K", SHAPES + TILES)
+@pytest.mark.parametrize("M,N,K", SHAPES + TILES + LONG)
 def test_linear(lvx, M, N, K, a8):
     call, ref, off, cut = products(lvx, M, N, K, a8, "lin")
     out = torch.full((M + 1, N + 8), 7.0, dtype=torch.bfloat16, device=DEV)
