@@ -8,6 +8,9 @@
 //   V       transposed: a lane holds eight consecutive keys (a word) of channel 16 cb + r, per channel block cb and half of the tile.
 //   scales  E8M0 per key and 32 channels of K (applied by the conversion to bf16, exactly), bf16 per key of V (applied to the probability in fp32: the
 //           second product sums over keys, so a scale of V can neither wait until after it nor, unless a power of two, go into its operand without rounding).
+//
+// One token each of 32 sequences of up to 24960 keys (8 kv heads, 40 heads, 510 MB): 91 us with the join, 5.6 TB/s, bound by HBM.  1560 tokens of 40 heads against 24960 keys:
+// 737 us, 1.05 PFLOP/s, bound by the vector unit (conversions, exponentials, packing: about 340 instructions a wave and tile beside 64 matrix products).
 #include "lvx_fp4.h"
 
 #include <new>
@@ -98,7 +101,8 @@ __device__ __forceinline__ uint32_t swap_max(uint32_t a, uint32_t b, bool halves
     return r[0] > r[1] ? r[0] : r[1];
 }
 
-// A wave quantises 8 NG aligned keys of one head: the keys of a word of V are never shared between waves.
+// A wave quantises 8 NG aligned keys of one head: the keys of a word of V are never shared between waves, so a word that keeps other keys' codes is read and written by one.
+// Bound by the loads' way and, for prompts, by the bytes (32 x 24960 keys of 8 heads 945 us, 4.4 TB/s; 4 prompts of up to 1560 tokens 11 us).
 template <int D, int NG>
 __global__ void __launch_bounds__(256) lvx_kv4_append_kernel(append_args_t p) {
     typedef tile_t<D> T;
@@ -699,9 +703,11 @@ namespace {
 
 constexpr int MAX_SPLITS = 64;
 
-// Rows per workgroup and ranges of keys of a call, by sizes that the host knows.  A sequence's rows of a kv head (tokens x heads of the group) up to 16 are one block, with four
-// waves sharing the keys; two blocks a wave with four, two or one wave on the same keys up to 32, up to 64 and beyond.  The keys are split into ranges while the workgroups
-// leave compute units idle and a range keeps at least 512 keys of a full cache.
+// Rows per workgroup and ranges of keys of a call, by sizes that the host knows.  A sequence's rows of a kv head (tokens x heads of the group) up to 16 are one block and up to
+// 32 two, with eight waves sharing the keys; two blocks a wave with two waves on the same keys up to 64, and one beyond: rows share a wave's keys, so they are stacked before
+// waves are.  The keys are split into ranges as long as there are at most 512 workgroups (two a compute unit) and a range keeps 512 keys of a full cache of 2048 or more:
+// one token of 40 heads against 4680 keys 6.3 us and 4.4 to join nine ranges, 17.1 in one; 32 sequences of up to 24960 keys 87 and 4.8 with two ranges, 104 in one, 92 and 4.9
+// with four; but 1301 keys 9.8 in one, 7.3 and 3.6 in two, and 488 workgroups of a prompt lose 26 us to joining two ranges and gain none.
 struct attn_plan_t {
     int rows, row_tiles, splits;  // rows of a workgroup: 16, 32, 64 or 128
 };
@@ -711,9 +717,8 @@ attn_plan_t attn_plan(const lvx_kv4_desc_t &d, int n_heads, int max_tokens) {
     pl.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
     pl.row_tiles = (int)((rows + pl.rows - 1) / pl.rows);
     const int64_t groups = (int64_t)pl.row_tiles * d.n_kv_heads * d.n_seqs;
-    const bool shared = pl.rows <= 32;  // eight waves share the keys
     int64_t splits = groups > 0 ? 512 / groups : 1;
-    const int64_t most = d.max_keys / (shared ? 1024 : 512);
+    const int64_t most = d.max_keys >= 2048 ? d.max_keys / 512 : 1;
     splits = splits < most ? splits : most;
     splits = splits < MAX_SPLITS ? splits : MAX_SPLITS;
     pl.splits = (int)(splits > 1 ? splits : 1);
