@@ -312,8 +312,8 @@ lvx_status_t lvx_linear_fp8_fp4(const void *dev_aq, int64_t lda, const float *de
  *
  * A call handles n_tokens new tokens in all, at most max_tokens of a sequence: sequence s has rows [dev_starts[s], dev_starts[s + 1]) (device int32 [n_seqs + 1];
  * NULL: max_tokens rows each, n_tokens = n_seqs * max_tokens), and dev_key_counts[s] (device int32 [n_seqs]) keys with its new tokens, so that its token i of n
- * is key dev_key_counts[s] - n + i.  Idle sequences have no rows.  Rows behind the last sequence are neither read nor written.  Counts beyond max_keys count
- * as max_keys; row ranges are cut to [0, n_tokens).
+ * is key dev_key_counts[s] - n + i.  Idle sequences have no rows.  Rows behind the last sequence are neither read nor written.  A count may pass
+ * max_keys: tokens behind the last place are not stored, and see the max_keys keys that there are.  Row ranges are cut to [0, n_tokens).
  *   lvx_kv4_append     quantises the new tokens' k and v ([n_tokens][ld], kv head h at columns h * head_dim) into their places; a place outside [0, max_keys) is not written.
  *   lvx_kv4_gather     keys [first_key, first_key + n_keys) of all sequences of a layer back as bf16 [n_seqs][n_keys][ld] (keys exact, values code * s rounded once); zeros
  *                      from a sequence's key count on.

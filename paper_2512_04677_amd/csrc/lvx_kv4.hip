@@ -53,9 +53,9 @@ struct batch_t {
     int32_t n_each, n_tokens;
 };
 struct span_t {
-    int first, n, count;
+    int first, n, count;  // count: as given, it may pass the slot
 };
-__device__ __forceinline__ span_t span_of(const batch_t &b, int s, int max_keys) {
+__device__ __forceinline__ span_t span_of(const batch_t &b, int s) {
     span_t r;
     if (b.starts != nullptr) {
         // whatever the array holds, no row outside [0, n_tokens) is touched
@@ -68,8 +68,13 @@ __device__ __forceinline__ span_t span_of(const batch_t &b, int s, int max_keys)
         r.first = s * b.n_each, r.n = b.n_each;
     }
     const int c = b.counts[s];
-    r.count = c < max_keys ? (c > -(1 << 30) ? c : -(1 << 30)) : max_keys;
+    r.count = c > -(1 << 30) ? c : -(1 << 30);
     return r;
+}
+// keys that token i of the span sees, of those that the slot holds
+__device__ __forceinline__ int keys_seen(const span_t &sp, int i, bool causal, int max_keys) {
+    const int c = causal ? sp.count - (sp.n - 1 - i) : sp.count;
+    return c < 0 ? 0 : c < max_keys ? c : max_keys;
 }
 
 struct append_args_t {
@@ -110,7 +115,7 @@ __global__ void __launch_bounds__(256) lvx_kv4_append_kernel(append_args_t p) {
     const int s = blockIdx.y, head = blockIdx.z * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (head >= p.kv_heads) return;
     const int c_raw = p.batch.counts[s];
-    const span_t sp = span_of(p.batch, s, p.max_keys);
+    const span_t sp = span_of(p.batch, s);
     const int64_t pos0 = (int64_t)c_raw - sp.n;  // position of the first token, before clipping
     const int64_t lo = pos0 > 0 ? pos0 : 0, hi = c_raw < p.max_keys ? c_raw : p.max_keys;
     const int64_t first = (lo & ~(8ll * NG - 1)) + 8ll * NG * blockIdx.x;
@@ -288,7 +293,7 @@ __global__ void __launch_bounds__(64 * WR * WK, 2) lvx_kv4_attention_kernel(attn
     const int r = lane & 15, g = lane >> 4;
     const int head = blockIdx.x % p.kv_heads, rt = (blockIdx.x / p.kv_heads) % p.row_tiles, split = blockIdx.x / p.kv_heads / p.row_tiles;
     const int s = blockIdx.y;
-    const span_t sp = span_of(p.batch, s, p.max_keys);
+    const span_t sp = span_of(p.batch, s);
     const int n_rows = sp.n * p.group;
     if (rt * 16 * RB * WR >= n_rows) return;
 
@@ -301,8 +306,7 @@ __global__ void __launch_bounds__(64 * WR * WK, 2) lvx_kv4_attention_kernel(attn
         const int row = row0 + 16 * b + r;
         const int i = row < n_rows ? row / p.group : sp.n - 1;
         const int head_of = head * p.group + (row < n_rows ? row % p.group : 0);
-        seen[b] = p.causal ? sp.count - (sp.n - 1 - i) : sp.count;
-        seen[b] = row < n_rows && seen[b] > 0 ? seen[b] : 0;
+        seen[b] = row < n_rows ? keys_seen(sp, i, p.causal, p.max_keys) : 0;
         const uint4 *src = reinterpret_cast<const uint4 *>(p.q + (int64_t)(sp.first + i) * p.ld_q + head_of * D + (D / 4) * g);
 #pragma unroll
         for (int j = 0; j < KS; ++j) {
@@ -312,9 +316,8 @@ __global__ void __launch_bounds__(64 * WR * WK, 2) lvx_kv4_attention_kernel(attn
     }
     // the keys that any of the workgroup's rows sees, and those that all of this wave's rows see
     const int last_row = (rt + 1) * 16 * RB * WR < n_rows ? (rt + 1) * 16 * RB * WR - 1 : n_rows - 1;
-    int most = p.causal ? sp.count - (sp.n - 1 - last_row / p.group) : sp.count;
-    most = most > 0 ? most : 0;
-    const int least = p.causal ? sp.count - (sp.n - 1 - row0 / p.group) : sp.count;
+    const int most = keys_seen(sp, last_row / p.group, p.causal, p.max_keys);
+    const int least = keys_seen(sp, row0 < n_rows ? row0 / p.group : sp.n - 1, p.causal, p.max_keys);
     const int tiles = (most + TILE - 1) / TILE, per = (tiles + p.splits - 1) / p.splits;
     const int t0 = split * per, t1 = t0 + per < tiles ? t0 + per : tiles;
 
@@ -370,7 +373,7 @@ __global__ void __launch_bounds__(64 * WR * WK, 2) lvx_kv4_attention_kernel(attn
                     for (int b = 0; b < RB; ++b) x[b][kp + h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[h], q[b][j], x[b][kp + h], 0, 0, 0);
             }
         }
-        // Registers bound how far ahead the next keys are requested: at once where a wave has one block of rows or the keys are shared, else when the scores are done with.
+        // Registers bound how far ahead the next keys are requested: behind the scores where waves share the keys, else when the scores are done with.
         if (WK > 1 && t + WK < t1) load_keys(t + WK);
         if (WK == 1) __builtin_amdgcn_s_setprio(0);
         // softmax; lane's keys: 32 (kb / 2) + 8 g + 4 (kb % 2) + i
@@ -539,7 +542,7 @@ __global__ void __launch_bounds__(256) lvx_kv4_combine_kernel(attn_args_t p) {
     constexpr int C = D / 64;
     const int lane = threadIdx.x & 63;
     const int s = blockIdx.y;
-    const span_t sp = span_of(p.batch, s, p.max_keys);
+    const span_t sp = span_of(p.batch, s);
     const int row = blockIdx.x * 4 + (threadIdx.x >> 6);
     if (row >= sp.n * p.n_heads) return;
     const int i = row / p.n_heads, head = row % p.n_heads;
@@ -570,8 +573,7 @@ __global__ void __launch_bounds__(256) lvx_kv4_combine_kernel(attn_args_t p) {
             for (int c = 0; c < C; ++c) o[c] += k0 + k < p.splits ? x[k][c] * f : 0.f;
         }
     }
-    const int seen = p.causal ? sp.count - (sp.n - 1 - i) : sp.count;
-    const float inv = seen > 0 ? 1.0f / sum : 0.f;
+    const float inv = keys_seen(sp, i, p.causal, p.max_keys) > 0 ? 1.0f / sum : 0.f;
     bf16_t *dst = p.out + (sp.first + i) * p.ld_out + head * D + C * lane;
     if (C == 2)
         *reinterpret_cast<uint32_t *>(dst) = pack_bf16x2(o[0] * inv, o[C - 1] * inv);
@@ -608,9 +610,6 @@ lvx_status_t check_call(const lvx_kv4_t *c, int32_t layer, const int32_t *starts
                 "without starts every sequence has max_tokens tokens: %d x %d are not %d", c->desc.n_seqs, max_tokens, n_tokens);
     return LVX_OK;
 }
-
-
-
 
 }  // namespace
 

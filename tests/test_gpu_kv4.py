@@ -237,3 +237,23 @@ def test_offsets_beyond_32_bits(lvx):
     ref, spread = np.einsum("jh,jhd->hd", p, dv), np.einsum("jh,jhd->hd", p, np.abs(dv))
     size = np.einsum("hd,jhd->jh", np.abs(S.to_f64(q).reshape(KV, D)), np.abs(dk)).max()
     assert np.all(np.abs(S.to_f64(out).reshape(KV, D) - ref) <= 2.0 ** -8 * np.abs(ref) + (2.0 ** -8 + 2.0 ** -16 + 2 * (D + 4) * 2.0 ** -24 * size) * spread)
+
+
+@pytest.mark.parametrize("group,n,count", [(1, 10, 75), (1, 40, 90), (8, 30, 1000), (2, 9, 2 ** 31 - 1)])
+def test_counts_beyond_the_slot(lvx, group, n, count):
+    """A count that passes the slot: every token sees the keys up to its own place, as append stored them, or all there are."""
+    KV, D, L = 2, 64, 70
+    tag = "over%d_%d_%d" % (group, n, count)
+    cache = lvx.KV4Cache(lvx.kv4_desc(1, 1, KV, D, L), DEV)
+    k, v, q = rows(L, KV * D, tag, "k"), rows(L, KV * D, tag, "v"), rows(n, KV * group * D, tag, "q")
+    lvx.lvx_kv4_append(cache, 0, k, v, i32([L]), max_tokens=L)
+    ws = torch.empty(lvx.lvx_kv4_attention_workspace_bytes(cache, KV * group, n), dtype=torch.uint8, device=DEV)
+    out, each = torch.empty_like(q), torch.empty_like(q)
+    lvx.lvx_kv4_attention(cache, 0, q, KV * group, 0.125, i32([count]), out, ws, max_tokens=n)
+    lvx.lvx_kv4_attention(cache, 0, q, KV * group, 0.125, i32([L]), each, ws, max_tokens=n, causal=False)
+    seen = [min(count - (n - 1 - i), L) for i in range(n)]
+    ref, spread, size = O.attention(S.to_f64(q).reshape(n, -1, D), decoded(k, KV, D), decoded_v(v, KV, D), 0.125, seen)
+    tol = 2.0 ** -8 * np.abs(ref) + (2.0 ** -8 + 2.0 ** -16 + 2 * (D + 4) * 2.0 ** -24 * size[..., None]) * spread
+    assert np.all(np.abs(S.to_f64(out).reshape(ref.shape) - ref) <= tol)
+    if min(seen) == L:
+        assert torch.equal(out, each)
