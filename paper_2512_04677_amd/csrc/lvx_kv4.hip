@@ -447,9 +447,13 @@ __global__ void __launch_bounds__(64 * WR * WK, 2) lvx_kv4_attention_kernel(attn
             float z[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) z[i] = y[i] * ((i & 1) ? bf16_hi(w[i >> 1]) : bf16_lo(w[i >> 1]));
-            if (masked) {  // a hidden key's scale may be anything
+            if (masked) {  // a hidden key's scale may be anything; a NaN that is seen stays, however small its probability
+                const int left = seen[b] - TILE * t - 8 * g;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) z[i] = y[i] == 0.f ? 0.f : z[i];
+                for (int kb = 0; kb < 4; ++kb)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (left <= 32 * (kb >> 1) + 4 * (kb & 1) + i) z[4 * kb + i] = 0.f;
             }
 #pragma unroll
             for (int h = 0; h < 2; ++h) {

@@ -257,3 +257,19 @@ def test_counts_beyond_the_slot(lvx, group, n, count):
     assert np.all(np.abs(S.to_f64(out).reshape(ref.shape) - ref) <= tol)
     if min(seen) == L:
         assert torch.equal(out, each)
+
+
+@pytest.mark.parametrize("H,n,L", [(1, 20, 64), (4, 20, 20), (8, 20, 90)])
+def test_unlikely_values_that_are_not_finite(lvx, H, n, L):
+    """A value that is no number reaches the tokens that see it though its probability underflows to zero, wherever its key lies in a tile."""
+    D = 128
+    cache = lvx.KV4Cache(lvx.kv4_desc(1, 1, 1, D, L), DEV)
+    q = rows(1, D, "unlikely").expand(n, D).repeat(1, H).contiguous()
+    k, v = rows(L, D, "unlikely_k", L).clone(), rows(L, D, "unlikely_v", L).clone()
+    k[L - 10] = (-10 * q[0, :D].float()).to(torch.bfloat16)      # a score near -10 * 128
+    v[L - 10] = float("nan")
+    lvx.lvx_kv4_append(cache, 0, k, v, i32([L]), max_tokens=L)
+    ws = torch.empty(lvx.lvx_kv4_attention_workspace_bytes(cache, H, n), dtype=torch.uint8, device=DEV)
+    out = torch.empty_like(q)
+    lvx.lvx_kv4_attention(cache, 0, q, H, 1.0, i32([L]), out, ws, max_tokens=n)
+    assert bool(torch.isfinite(out[:n - 10]).all()) and bool(torch.isnan(out[n - 10:]).all())
