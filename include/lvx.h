@@ -278,8 +278,8 @@ lvx_status_t lvx_layernorm_modulate(const void *dev_x, int64_t ldx, const float 
  *   x bf16 or NULL (0); resid bf16, or fp32 with resid_is_f32 = 1 (strides in fp32 elements), or NULL (0), not both NULL; gain fp32 [d] or NULL (1).
  *   dev_sum (may be NULL; needs a residual): h in the residual's type.  dev_y: bf16.  Each output may be the buffer of an input of the same type
  *   and stride.  d % 8 == 0, d <= 16384, strides % 8 == 0, fewer than 2^22 tokens.
- * lvx_rmsnorm_residual_fp8: y leaves as E4M3 codes with one fp32 scale a row: scale = max|y| / 448 (1 for a zero row), code =
- *   E4M3(y * (448 / max|y|)), nearest-even: what lvx_linear_fp8_fp4 takes.  d % 16 == 0, ldq % 16 == 0.  A row that holds a NaN or an
+ * lvx_rmsnorm_residual_fp8: y leaves as E4M3 codes with one fp32 scale a row: scale = max|y| / 448 (1 for a zero row, at least 2^-126),
+ *   code = E4M3(y * (448 / max|y|)), nearest-even: what lvx_linear_fp8_fp4 takes.  d % 16 == 0, ldq % 16 == 0.  A row that holds a NaN or an
  *   infinity has a NaN scale. */
 lvx_status_t lvx_rmsnorm_residual(const void *dev_x, int64_t ldx, const void *dev_resid, int64_t ldr, int32_t resid_is_f32, const float *dev_gain,
                                   float eps, int32_t n_tokens, int32_t d, void *dev_sum, int64_t ld_sum, void *dev_y, int64_t ldy,

@@ -128,8 +128,10 @@ __global__ void __launch_bounds__(T < 256 ? 256 : T) lvx_rmsnorm_residual_kernel
     if (!FP8) return;
 
     const float amax = __uint_as_float(row_max<T>(most, lds_max));
-    const float inv = amax == 0.f ? 0.f : E4M3_MAX / amax;
-    if (t == 0) p.row_scales[row] = amax == 0.f ? 1.0f : amax / E4M3_MAX;
+    // a scale below the normal numbers would lose bits, and its inverse be infinite
+    const bool tiny = amax < E4M3_MAX * 0x1p-126f;
+    const float inv = amax == 0.f ? 0.f : tiny ? 0x1p126f : E4M3_MAX / amax;
+    if (t == 0) p.row_scales[row] = amax == 0.f ? 1.0f : tiny ? 0x1p-126f : amax / E4M3_MAX;
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
         const int c = t + T * i;

@@ -93,3 +93,14 @@ def test_norm_zero_and_non_finite_rows(lvx):
     y = torch.empty(n, d, dtype=torch.bfloat16, device=DEV)
     lvx.lvx_rmsnorm_residual(x, r, g, 1e-6, y)
     assert bool(torch.isnan(y[2]).all()) and bool(torch.isnan(y[3, 200])) and not bool(y[1].any())
+
+
+@pytest.mark.parametrize("d", [64, 2064, 16384])
+def test_tiny_rows_to_8_bits(lvx, d):
+    """Rows whose scale max|y| / 448 would be no normal number: it stays at 2^-126, and multiples of it up to 448 are exact (eps 1: y is h)."""
+    r = torch.zeros(3, d, device=DEV)
+    r[0, 3], r[0, 9], r[1, d - 1] = 2.0 ** -126, -3 * 2.0 ** -126, 416 * 2.0 ** -126
+    q, sc = torch.full((3, d), 77, dtype=torch.uint8, device=DEV), torch.empty(3, device=DEV)
+    lvx.lvx_rmsnorm_residual_fp8(None, r, None, 1.0, q, sc)
+    assert np.array_equal(e4m3_decode(q.cpu().numpy()) * S.to_f64(sc)[:, None], S.to_f64(r))
+    assert S.to_f64(sc).tolist() == [2.0 ** -126, 2.0 ** -126, 1.0]
