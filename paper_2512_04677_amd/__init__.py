@@ -163,6 +163,23 @@ def _stream():
     return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
+def _stream_of(t):
+    """The same for a launch that works on t, which has to lie on that device: another device's (or the host's) address would fault the kernel."""
+    import torch
+    d = t.get_device()
+    if d < 0 or d != torch._C._cuda_getDevice():
+        raise LvxError(1, f"a tensor lies on {t.device}, not on the current device")
+    return torch._C._cuda_getCurrentRawStream(d)
+
+
+def _check_i32(t, n, like):
+    """Lengths and row ranges are read on the device as n int32 in a row."""
+    import torch
+    if t.dtype is not torch.int32 or t.numel() < n or not t.is_contiguous() or t.get_device() != like.get_device():
+        raise LvxError(1, f"key counts and starts are contiguous int32 tensors on the data's device, here of at least {n} elements")
+    return t.data_ptr()
+
+
 def version():
     return load().lvx_version().decode()
 
@@ -350,7 +367,7 @@ def lvx_rmsnorm_residual(x, resid, gain, eps, y, sum_out=None):
     _check_like(resid, sum_out)
     a = _norm_args(x, resid, gain, eps, sum_out)
     if a[7]:
-        _check(load().lvx_rmsnorm_residual(*a, y.data_ptr(), y.stride(0), _stream()))
+        _check(load().lvx_rmsnorm_residual(*a, y.data_ptr(), y.stride(0), _stream_of(y)))
 
 
 def lvx_rmsnorm_residual_fp8(x, resid, gain, eps, q, row_scales, sum_out=None):
@@ -358,7 +375,7 @@ def lvx_rmsnorm_residual_fp8(x, resid, gain, eps, q, row_scales, sum_out=None):
     _check_like(resid, sum_out)
     a = _norm_args(x, resid, gain, eps, sum_out)
     if a[7]:
-        _check(load().lvx_rmsnorm_residual_fp8(*a, q.data_ptr(), q.stride(0), row_scales.data_ptr(), _stream()))
+        _check(load().lvx_rmsnorm_residual_fp8(*a, q.data_ptr(), q.stride(0), row_scales.data_ptr(), _stream_of(q)))
 
 
 def _check_like(resid, sum_out):
@@ -374,7 +391,7 @@ def lvx_fp4_quantize(x, q=None, scales=None):
         q = torch.empty((rows, cols // 2), dtype=torch.uint8, device=x.device)
     if scales is None:
         scales = torch.empty((rows, cols // 32), dtype=torch.uint8, device=x.device)
-    _check(load().lvx_fp4_quantize(_ptr(x), x.stride(0), rows, cols, _ptr(q), q.stride(0), _ptr(scales), scales.stride(0), _stream()))
+    _check(load().lvx_fp4_quantize(_ptr(x), x.stride(0), rows, cols, _ptr(q), q.stride(0), _ptr(scales), scales.stride(0), _stream_of(x)))
     return q, scales
 
 
@@ -383,7 +400,7 @@ def lvx_linear_fp4(a, wq, w_scales, c, epi=EPI_STORE, resid=None, gate=None):
     M, K = a.shape
     if M:
         _check(load().lvx_linear_fp4(a.data_ptr(), a.stride(0), wq.data_ptr(), wq.stride(0), w_scales.data_ptr(), w_scales.stride(0), c.data_ptr(),
-                                     c.stride(0), M, wq.shape[0], K, epi, _ptr(resid), 0 if resid is None else resid.stride(0), _ptr(gate), _stream()))
+                                     c.stride(0), M, wq.shape[0], K, epi, _ptr(resid), 0 if resid is None else resid.stride(0), _ptr(gate), _stream_of(c)))
 
 
 def lvx_linear_fp8_fp4(aq, row_scales, wq, w_scales, c, epi=EPI_STORE, resid=None, gate=None):
@@ -392,7 +409,7 @@ def lvx_linear_fp8_fp4(aq, row_scales, wq, w_scales, c, epi=EPI_STORE, resid=Non
     if M:
         _check(load().lvx_linear_fp8_fp4(aq.data_ptr(), aq.stride(0), row_scales.data_ptr(), wq.data_ptr(), wq.stride(0), w_scales.data_ptr(),
                                          w_scales.stride(0), c.data_ptr(), c.stride(0), M, wq.shape[0], K, epi, _ptr(resid),
-                                         0 if resid is None else resid.stride(0), _ptr(gate), _stream()))
+                                         0 if resid is None else resid.stride(0), _ptr(gate), _stream_of(c)))
 
 
 def kv4_desc(n_layers, n_seqs, n_kv_heads, head_dim, max_keys):
@@ -433,15 +450,20 @@ def lvx_kv4_append(cache, layer, k, v, key_counts, starts=None, max_tokens=1, n_
         raise LvxError(2, "k and v must share their row stride")
     n = k.shape[0] if n_tokens is None else n_tokens
     if n:
-        _check(load().lvx_kv4_append(cache.handle, layer, k.data_ptr(), v.data_ptr(), ld, _ptr(starts), n, max_tokens, key_counts.data_ptr(), _stream()))
+        _check(load().lvx_kv4_append(cache.handle, layer, k.data_ptr(), v.data_ptr(), ld,
+                                     None if starts is None else _check_i32(starts, cache.desc.n_seqs + 1, k), n, max_tokens,
+                                     _check_i32(key_counts, cache.desc.n_seqs, k), _stream_of(k)))
 
 
 def lvx_kv4_gather(cache, layer, key_counts, k_out, v_out, first_key=0):
-    """k_out, v_out: bf16 [n_seqs][n_keys][kv heads * head_dim], contiguous but for a padded row, of the same strides."""
+    """k_out, v_out: bf16 [n_seqs][n_keys][kv heads * head_dim], contiguous but for a padded row, of the same strides (no keys: nothing is done)."""
     for t in (k_out, v_out):
-        if t.dim() != 3 or t.shape[0] != cache.desc.n_seqs or t.stride() != k_out.stride() or t.stride(0) != t.shape[1] * t.stride(1):
+        if t.dim() != 3 or t.shape[0] != cache.desc.n_seqs or t.shape != k_out.shape or t.stride() != k_out.stride() or (
+                t.shape[0] > 1 and t.shape[1] > 0 and t.stride(0) != t.shape[1] * t.stride(1)):
             raise LvxError(2, "the outputs are [n_seqs][n_keys][columns] of the same strides")
-    _check(load().lvx_kv4_gather(cache.handle, layer, first_key, k_out.shape[1], _ptr(key_counts), _ptr(k_out), _ptr(v_out), k_out.stride(1), _stream()))
+    if k_out.shape[1]:
+        _check(load().lvx_kv4_gather(cache.handle, layer, first_key, k_out.shape[1], _check_i32(key_counts, cache.desc.n_seqs, k_out), _ptr(k_out), _ptr(v_out),
+                                     k_out.stride(1), _stream_of(k_out)))
 
 
 def lvx_kv4_attention_workspace_bytes(cache, n_heads, max_tokens):
@@ -455,8 +477,10 @@ def lvx_kv4_attention(cache, layer, q, n_heads, scale, key_counts, out, workspac
     """q, out: bf16 [n_tokens][heads * head_dim] (no tokens: nothing is done); workspace: lvx_kv4_attention_workspace_bytes(cache, n_heads, max_tokens) bytes."""
     n = q.shape[0] if n_tokens is None else n_tokens
     if n:
-        _check(load().lvx_kv4_attention(cache.handle, layer, q.data_ptr(), q.stride(0), n_heads, _ptr(starts), n, max_tokens, key_counts.data_ptr(),
-                                        1 if causal else 0, scale, out.data_ptr(), out.stride(0), workspace.data_ptr(), workspace.nbytes, _stream()))
+        _check(load().lvx_kv4_attention(cache.handle, layer, q.data_ptr(), q.stride(0), n_heads,
+                                        None if starts is None else _check_i32(starts, cache.desc.n_seqs + 1, q), n, max_tokens,
+                                        _check_i32(key_counts, cache.desc.n_seqs, q), 1 if causal else 0, scale, out.data_ptr(), out.stride(0),
+                                        workspace.data_ptr(), workspace.nbytes, _stream_of(q)))
 
 
 class StageHandle:

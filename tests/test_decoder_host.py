@@ -136,3 +136,35 @@ def test_workspace_never_shrinks_with_the_tokens():
 def test_python_binding_refuses():
     with pytest.raises(lvx.LvxError):
         lvx.KV4Cache(lvx.kv4_desc(1, 1, 1, 96, 64), "cpu")
+
+
+def test_python_binding_refuses_what_would_fault():
+    """Tensors on the host, lengths of another type, too few of them or with gaps: refused before a launch."""
+    import torch
+    bf, i32 = torch.bfloat16, torch.int32
+    w, s = torch.zeros(64, 32, dtype=torch.uint8), torch.zeros(64, 2, dtype=torch.uint8)
+    x, c = torch.zeros(3, 64, dtype=bf), torch.zeros(3, 64, dtype=bf)
+    for f in (lambda: lvx.lvx_linear_fp4(x, w, s, c), lambda: lvx.lvx_rmsnorm_residual(x, None, None, 1e-6, c), lambda: lvx.lvx_fp4_quantize(x)):
+        with pytest.raises(lvx.LvxError, match="current device"):
+            f()
+
+    class Stub:
+        desc, handle = lvx.kv4_desc(1, 3, 1, 64, 64), handle(n_layers=1, n_kv_heads=1, head_dim=64, max_keys=64)
+
+    ws, good = torch.zeros(256, dtype=torch.uint8), torch.ones(3, dtype=i32)
+    out = torch.zeros(3, 4, 64, dtype=bf)
+    for counts, starts in ((torch.ones(3, dtype=torch.int64), None), (torch.ones(2, dtype=i32), None), (torch.ones(3, 2, dtype=i32)[:, 0], None),
+                           (good, torch.zeros(3, dtype=i32)), (good, torch.zeros(4))):
+        with pytest.raises(lvx.LvxError, match="int32"):
+            lvx.lvx_kv4_append(Stub, 0, x, x, counts, starts=starts)
+        with pytest.raises(lvx.LvxError, match="int32"):
+            lvx.lvx_kv4_attention(Stub, 0, x, 1, 0.1, counts, c, ws, starts=starts)
+        if starts is None:
+            with pytest.raises(lvx.LvxError, match="int32"):
+                lvx.lvx_kv4_gather(Stub, 0, counts, out, out.clone())
+    with pytest.raises(lvx.LvxError, match="current device"):
+        lvx.lvx_kv4_append(Stub, 0, x, x, good)
+    with pytest.raises(lvx.LvxError, match="strides"):
+        lvx.lvx_kv4_gather(Stub, 0, good, out, out[:, :2])
+    lvx.lvx_kv4_gather(Stub, 0, good, out[:, :0], out[:, :0])
+    lvx.lvx_rmsnorm_residual(x[:0], None, None, 1e-6, c[:0])
