@@ -10,8 +10,9 @@
 //           second product sums over keys, so a scale of V can neither wait until after it nor, unless a power of two, go into its operand without rounding).
 //
 // One token each of 32 sequences of up to 24960 keys (8 kv heads, 40 heads, 510 MB): 91 us with the join, 5.6 TB/s, bound by HBM.  1560 tokens of 40 heads against 24960 keys:
-// 737 us, 1.05 PFLOP/s, bound by the vector unit (conversions, exponentials, packing: about 340 instructions a wave and tile beside 64 matrix products).
+// 734 to 753 us on different cards, 1.05 PFLOP/s, bound by the vector unit (conversions, exponentials, packing: about 340 instructions a wave and tile beside 64 matrix products).
 #include "lvx_fp4.h"
+#include "lvx_kv4_rules.h"
 
 #include <new>
 
@@ -291,7 +292,8 @@ __global__ void __launch_bounds__(64 * WR * WK, 2) lvx_kv4_attention_kernel(attn
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wr = wave % WR, wk = wave / WR;
     const int r = lane & 15, g = lane >> 4;
-    const int head = blockIdx.x % p.kv_heads, rt = (blockIdx.x / p.kv_heads) % p.row_tiles, split = blockIdx.x / p.kv_heads / p.row_tiles;
+    // the last rows first: a causal prompt's last see the most keys
+    const int head = blockIdx.x % p.kv_heads, rt = p.row_tiles - 1 - (blockIdx.x / p.kv_heads) % p.row_tiles, split = blockIdx.x / p.kv_heads / p.row_tiles;
     const int s = blockIdx.y;
     const span_t sp = span_of(p.batch, s);
     const int n_rows = sp.n * p.group;
@@ -449,7 +451,7 @@ __global__ void __launch_bounds__(64 * WR * WK, 2) lvx_kv4_attention_kernel(attn
             for (int i = 0; i < 16; ++i) z[i] = y[i] * ((i & 1) ? bf16_hi(w[i >> 1]) : bf16_lo(w[i >> 1]));
             if (masked) {  // a hidden key's scale may be anything; a NaN that is seen stays, however small its probability
                 int left = seen[b] - TILE * t - 8 * g;
-                asm volatile("" : "+v"(left));  // compared afresh: the conditions above, kept until here, cost the prompts' kernel 50 of 785 us
+                asm volatile("" : "+v"(left));  // compared afresh: the conditions above, kept until here, cost the kernel for prompts 50 of 785 us
 #pragma unroll
                 for (int kb = 0; kb < 4; ++kb)
 #pragma unroll
@@ -705,32 +707,8 @@ extern "C" lvx_status_t lvx_kv4_gather(const lvx_kv4_t *cache, int32_t layer, in
 
 namespace {
 
-constexpr int MAX_SPLITS = 64;
-
-// Rows per workgroup and ranges of keys of a call, by sizes that the host knows.  A sequence's rows of a kv head (tokens x heads of the group) up to 16 are one block and up to
-// 32 two, with eight waves sharing the keys; two blocks a wave with two waves on the same keys up to 64, and one beyond: rows share a wave's keys, so they are stacked before
-// waves are.  The keys are split into ranges as long as there are at most 512 workgroups (two a compute unit) and a range keeps 512 keys of a full cache of 2048 or more:
-// one token of 40 heads against 4680 keys 6.3 us and 4.4 to join nine ranges, 17.1 in one; 32 sequences of up to 24960 keys 87 and 4.8 with two ranges, 104 in one, 92 and 4.9
-// with four; but 1301 keys 9.8 in one, 7.3 and 3.6 in two, and 488 workgroups of a prompt lose 26 us to joining two ranges and gain none.
-struct attn_plan_t {
-    int rows, row_tiles, splits;  // rows of a workgroup: 16, 32, 64 or 128
-};
-attn_plan_t attn_plan(const lvx_kv4_desc_t &d, int n_heads, int max_tokens) {
-    attn_plan_t pl;
-    const int64_t rows = (int64_t)max_tokens * (n_heads / d.n_kv_heads);
-    pl.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
-    pl.row_tiles = (int)((rows + pl.rows - 1) / pl.rows);
-    const int64_t groups = (int64_t)pl.row_tiles * d.n_kv_heads * d.n_seqs;
-    int64_t splits = groups > 0 ? 512 / groups : 1;
-    const int64_t most = d.max_keys >= 2048 ? d.max_keys / 512 : 1;
-    splits = splits < most ? splits : most;
-    splits = splits < MAX_SPLITS ? splits : MAX_SPLITS;
-    pl.splits = (int)(splits > 1 ? splits : 1);
-    return pl;
-}
-
 template <int D>
-void attn_launch(const attn_plan_t &pl, const attn_args_t &p, dim3 grid, hipStream_t stream) {
+void attn_launch(const lvx_kv4_plan_t &pl, const attn_args_t &p, dim3 grid, hipStream_t stream) {
     if (pl.rows == 16)
         hipLaunchKernelGGL((lvx_kv4_attention_kernel<D, 1, 1, 8>), grid, dim3(512), 0, stream, p);
     else if (pl.rows == 32)
@@ -741,11 +719,9 @@ void attn_launch(const attn_plan_t &pl, const attn_args_t &p, dim3 grid, hipStre
         hipLaunchKernelGGL((lvx_kv4_attention_kernel<D, 2, 4, 1>), grid, dim3(256), 0, stream, p);
 }
 
+// for the partial outputs of any call of up to max_tokens tokens a sequence
 uint64_t attn_scratch(const lvx_kv4_desc_t &d, int n_heads, int max_tokens) {
-    const attn_plan_t pl = attn_plan(d, n_heads, max_tokens);
-    if (pl.splits == 1) return 0;
-    const uint64_t rows = (uint64_t)max_tokens * d.n_seqs * n_heads;
-    return pl.splits * rows * (4ull * d.head_dim + 8);
+    return lvx_kv4_partial_rows(d.n_seqs, d.max_keys, n_heads, max_tokens) * (4ull * d.head_dim + 8);
 }
 
 }  // namespace
@@ -755,15 +731,8 @@ extern "C" size_t lvx_kv4_attention_workspace_bytes(const lvx_kv4_t *cache, int3
         lvx_fail(LVX_ERR_INVALID_ARG, "cache handle is NULL, heads %d are no positive multiple of the kv heads, or tokens %d are negative", n_heads, max_tokens);
         return 0;
     }
-    // fewer tokens may be split further: the workspace of a longer call serves every shorter one
-    uint64_t n = 256;
-    for (int32_t t = 1; t <= max_tokens; ++t) {
-        const uint64_t its = attn_scratch(cache->desc, n_heads, t);
-        n = n > its ? n : its;
-        const attn_plan_t pl = attn_plan(cache->desc, n_heads, t);
-        if (pl.rows == 128 && pl.splits == 1) break;  // and none is from here on
-    }
-    return (size_t)n;
+    const uint64_t n = attn_scratch(cache->desc, n_heads, max_tokens);
+    return (size_t)(n > 256 ? n : 256);
 }
 
 extern "C" lvx_status_t lvx_kv4_attention(const lvx_kv4_t *cache, int32_t layer, const void *dev_q, int64_t ld_q, int32_t n_heads, const int32_t *dev_starts,
@@ -780,7 +749,7 @@ extern "C" lvx_status_t lvx_kv4_attention(const lvx_kv4_t *cache, int32_t layer,
                 "row strides must be multiples of 8 and at least heads * head_dim");
     LVX_REQUIRE((int64_t)max_tokens * n_heads <= INT32_MAX / 2, LVX_ERR_SHAPE, "%d tokens of %d heads are too many rows", max_tokens, n_heads);
     if (n_tokens == 0) return LVX_OK;
-    const attn_plan_t pl = attn_plan(d, n_heads, max_tokens);
+    const lvx_kv4_plan_t pl = lvx_kv4_plan(d.n_seqs, d.n_kv_heads, d.max_keys, n_heads, max_tokens);
     LVX_REQUIRE(workspace_bytes >= attn_scratch(d, n_heads, max_tokens), LVX_ERR_SHAPE, "workspace of %zu bytes, %llu needed", workspace_bytes,
                 (unsigned long long)attn_scratch(d, n_heads, max_tokens));
     const int64_t grid_x = (int64_t)pl.splits * pl.row_tiles * d.n_kv_heads;

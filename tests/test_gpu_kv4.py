@@ -273,3 +273,34 @@ def test_unlikely_values_that_are_not_finite(lvx, H, n, L):
     out = torch.empty_like(q)
     lvx.lvx_kv4_attention(cache, 0, q, H, 1.0, i32([L]), out, ws, max_tokens=n)
     assert bool(torch.isfinite(out[:n - 10]).all()) and bool(torch.isnan(out[n - 10:]).all())
+
+
+# sequences, kv heads, heads of a group, tokens, keys; rows of a workgroup, whether the keys are split (tests/test_kv4_rules.py holds the rule to them)
+FORMS = [(3, 1, 3, 5, 129, 16, False), (1, 1, 1, 1, 3000, 16, True), (1, 2, 3, 700, 3000, 32, False), (1, 1, 3, 700, 9000, 32, True),
+         (1, 8, 8, 130, 130, 64, False), (1, 2, 3, 1500, 9000, 64, True), (16, 8, 5, 64, 130, 128, False), (2, 8, 8, 130, 9000, 128, True)]
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("S_,KV,group,n,L,rows_,splits", FORMS)
+def test_every_form(lvx, D, S_, KV, group, n, L, rows_, splits):
+    """Every form of the kernel with one range of keys and with several, on ragged tokens and lengths; some tokens of each sequence against the oracle."""
+    tag, H = "form%d_%d_%d_%d_%d" % (D, KV, group, n, L), KV * group
+    new = [max(1, n - 5 * s) for s in range(S_)]
+    counts = [max(1, L - 40 * s) if s % 3 < 2 else new[s] // 2 for s in range(S_)]
+    cache, kv = make(lvx, S_, KV, D, L, counts, tag)
+    starts = [0] + list(np.cumsum(new))
+    q = rows(sum(new), H * D, tag, "q")
+    for causal in (True, False):
+        out = torch.full((sum(new) + 1, H * D), 7.0, dtype=torch.bfloat16, device=DEV)
+        ws = torch.empty(lvx.lvx_kv4_attention_workspace_bytes(cache, H, n) + 64, dtype=torch.uint8, device=DEV).fill_(0xff)
+        for _ in range(2):
+            lvx.lvx_kv4_attention(cache, 1, q, H, 1 / math.sqrt(D), i32(counts), out, ws[:-64], starts=i32(starts), max_tokens=n, causal=causal)
+        assert bool((ws[-64:] == 0xff).all()) and bool((out[-1] == 7).all()) and bool(torch.isfinite(out).all())
+        for s in range(S_):
+            at = sorted({0, 1, new[s] // 3, new[s] // 2, new[s] - 1} & set(range(new[s])))
+            sel = [starts[s] + i for i in at]
+            seen = [counts[s] - (new[s] - 1 - i) if causal else counts[s] for i in at]
+            ref, spread, size = O.attention(S.to_f64(q[sel]).reshape(-1, H, D), *kv[s], 1 / math.sqrt(D), seen)
+            tol = 2.0 ** -8 * np.abs(ref) + (2.0 ** -8 + 2.0 ** -16 + 2 * (D + 4) * 2.0 ** -24 * size[..., None]) * spread
+            err = np.abs(S.to_f64(out[sel]).reshape(ref.shape) - ref)
+            assert np.all(err <= tol), (s, causal, float((err - tol).max()))
