@@ -5,6 +5,7 @@
 //
 // Weights stay exact: a code times its scale is a bf16 number, and its products with a bf16 or E4M3 value are exact in fp32.
 #include "lvx_fp4.h"
+#include "lvx_fp4_rules.h"
 
 namespace {
 
@@ -81,8 +82,7 @@ __device__ __forceinline__ void fp4_row_scales(const fp4_args_t &p, int m0, floa
     }
 }
 
-// How the rows of A become operands: bf16 as they are; E4M3 widened to bf16 (exact, every product is); or E4M3 against E2M1 in one instruction.
-enum { A_BF16 = 0, A_WIDEN = 1, A_NATIVE = 2 };
+enum { A_BF16 = LVX_FP4_A_BF16, A_WIDEN = LVX_FP4_A_WIDEN, A_NATIVE = LVX_FP4_A_NATIVE };
 
 // Matrix products of a step of 128 channels: w[b] the codes of 16 columns, s[b] their scale as a byte (native) or as fp32 bits (widened codes), a[c] the operands of 16 rows.
 template <int MODE, int MB, int NB>
@@ -357,26 +357,27 @@ __global__ void __launch_bounds__(512) lvx_fp4_resident_kernel(fp4_args_t p) {
     }
 }
 
-// ---- many rows: tiles of 32 MBW rows and 128 columns ---------------------------------------------------------------------
-// Bound by the matrix cores and the LDS.  Eight waves: two groups over K, every second pair of steps each, of two by two waves (half the rows, half the columns).  Rows
+// ---- many rows: tiles of 32 MBW rows and 256 / KG columns -----------------------------------------------------------------
+// Bound by the matrix cores and the LDS.  Eight waves: KG groups over K, every KG-th pair of steps each, of two waves over the rows and one or two over the columns.  Rows
 // and weights come by direct loads to LDS, RING steps and a pair or two of steps ahead: a stage of the weights is a pair, because a weight row's 128 channels are half a
 // cache line and halves cost as much as lines.  A wave reads the next step's operands into registers while it multiplies this one's.  16-byte chunk c of a row of CH
 // chunks lies at c ^ (row % CH), so that the sixteen rows of an operand fall into different banks.  544 8-bit rows x 5120 x 13824: 52 us, 1.49 PFLOP/s; of that the loop without
 // loads, reads and products is 26, the reads of LDS 16, the products 19, and they overlap only in part.
-template <int MODE, int MBW, int RING>
+template <int MODE, int MBW, int KG, int RING>
 __global__ void __launch_bounds__(512) lvx_fp4_tile_kernel(fp4_args_t p) {
     constexpr int NB = 4, AV = MODE == A_BF16 ? 4 : 2, ROW = MODE == A_BF16 ? 256 : 128, CH = ROW / 16, MT = 32 * MBW;
-    constexpr int A_STAGE = MT * ROW, W_STAGE = 128 * 128, A_PER = 1024 / ROW;  // A_PER: rows of an instruction
-    constexpr int DA = A_STAGE / 4096, DW = 4;                                  // requests of a wave per stage
-    extern __shared__ char lds[];  // [2][RING] stages of rows, [2][2] of weights, the scales; then the partial sums
-    uint32_t *scales = reinterpret_cast<uint32_t *>(lds + 2 * RING * A_STAGE + 4 * W_STAGE);  // [128][PANEL]
+    constexpr int WAVES = 8 / KG, NW = WAVES / 2, COLS = 64 * NW;               // waves of a group: two over the rows, NW over the columns
+    constexpr int A_STAGE = MT * ROW, W_STAGE = COLS * 128, A_PER = 1024 / ROW;  // A_PER: rows of an instruction
+    constexpr int DA = A_STAGE / (1024 * WAVES), DW = 4;                         // requests of a wave per stage
+    extern __shared__ char lds[];  // [KG][RING] stages of rows, [KG][2] of weights, the scales; then the partial sums
+    uint32_t *scales = reinterpret_cast<uint32_t *>(lds + KG * RING * A_STAGE + KG * 2 * W_STAGE);  // [COLS][PANEL]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int kg = wave >> 2, mw = (wave >> 1) & 1, nw = wave & 1, in_group = wave & 3;
+    const int kg = wave / WAVES, in_group = wave % WAVES, mw = in_group / NW, nw = in_group % NW;
     const int r = lane & 15, g = lane >> 4;
-    const int n0 = blockIdx.x * 128, m0 = blockIdx.y * MT;
-    const int steps = (p.K + 127) / 128, rounds = (steps + 3) / 4;
+    const int n0 = blockIdx.x * COLS, m0 = blockIdx.y * MT;
+    const int steps = (p.K + 127) / 128, rounds = (steps + 2 * KG - 1) / (2 * KG);
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
-    const uint32_t lds_a = lds0 + kg * RING * A_STAGE, lds_w = lds0 + 2 * RING * A_STAGE + kg * 2 * W_STAGE;
+    const uint32_t lds_a = lds0 + kg * RING * A_STAGE, lds_w = lds0 + KG * RING * A_STAGE + kg * 2 * W_STAGE;
 
     // this wave's share of its group's requests: rows past the end repeat the last one (they are multiplied and not stored)
     uint32_t a_off[DA], a_col[DA], w_off[DW], w_col[DW];
@@ -394,8 +395,8 @@ __global__ void __launch_bounds__(512) lvx_fp4_tile_kernel(fp4_args_t p) {
     }
     const char *a_base = p.A + (int64_t)m0 * p.lda;
     const uint8_t *w_base = p.W + (int64_t)n0 * p.ldw;
-    // the group's j-th step: pairs kg, kg + 2, ... of two steps each
-    auto step = [&](int j) { return 2 * (kg + 2 * (j >> 1)) + (j & 1); };
+    // the group's j-th step: pairs kg, kg + KG, ... of two steps each
+    auto step = [&](int j) { return 2 * (kg + KG * (j >> 1)) + (j & 1); };
     // of the last stage, chunks behind K are not read: the row's first is, in their place, and not used
     auto stage_a = [&](int j) {
         const int t = step(j);
@@ -405,22 +406,23 @@ __global__ void __launch_bounds__(512) lvx_fp4_tile_kernel(fp4_args_t p) {
             lvx_dma16(a_base, a_off[i] + (a_col[i] < chunks ? (uint32_t)t * ROW + 16 * a_col[i] : 0), to + (in_group * DA + i) * 1024);
     };
     auto stage_w = [&](int j) {  // of the pair that begins with step j
-        const int q = kg + 2 * (j >> 1);
+        const int q = kg + KG * (j >> 1);
         const uint32_t chunks = (uint32_t)((p.K - 256 * q) / 32), to = lds_w + ((j >> 1) & 1) * W_STAGE;
 #pragma unroll
         for (int i = 0; i < DW; ++i)
             lvx_dma16(w_base, w_off[i] + (w_col[i] < chunks ? (uint32_t)q * 128 + 16 * w_col[i] : 0), to + (in_group * DW + i) * 1024);
     };
-    // the scales of the PANEL steps (of both groups) from the group's step j on: 16 bytes = four steps of a column a piece
+    // the scales of the PANEL steps (of all groups) from the groups' step j on: 16 bytes = four steps of a column a piece
     auto load_scales = [&](int j) {
-        const int b0 = 8 * j, row_bytes = p.K / LVX_FP4_GROUP;
-        constexpr int PIECES = 128 * (PANEL / 4) / 512;
+        const int b0 = 4 * KG * j, row_bytes = p.K / LVX_FP4_GROUP;
+        constexpr int ALL = COLS * (PANEL / 4), PIECES = (ALL + 511) / 512;
         uint4 v[PIECES];
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
             const int piece = threadIdx.x + 512 * i, row = piece / (PANEL / 4), at = b0 + 16 * (piece % (PANEL / 4));
             const uint8_t *src = p.S + (n0 + row < p.N ? n0 + row : p.N - 1) * p.lds + at;
             uint32_t e[4] = {0, 0, 0, 0};
+            if (ALL % 512 != 0 && piece >= ALL) continue;
             if (at + 16 <= row_bytes) {
                 __builtin_memcpy(e, src, 16);
             } else if (at < row_bytes) {
@@ -440,6 +442,7 @@ __global__ void __launch_bounds__(512) lvx_fp4_tile_kernel(fp4_args_t p) {
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
             const int piece = threadIdx.x + 512 * i;
+            if (ALL % 512 != 0 && piece >= ALL) continue;
             *reinterpret_cast<uint4 *>(scales + (piece / (PANEL / 4)) * PANEL + 4 * (piece % (PANEL / 4))) = v[i];
         }
     };
@@ -457,7 +460,7 @@ __global__ void __launch_bounds__(512) lvx_fp4_tile_kernel(fp4_args_t p) {
         const int t = step(j);
         if (t >= steps) return;
         const char *a_src = lds + kg * RING * A_STAGE + (j % RING) * A_STAGE + (mw * 16 * MBW + r) * ROW;
-        const char *w_src = lds + 2 * RING * A_STAGE + (kg * 2 + ((j >> 1) & 1)) * W_STAGE + (nw * 64 + r) * 128;
+        const char *w_src = lds + KG * RING * A_STAGE + (kg * 2 + ((j >> 1) & 1)) * W_STAGE + (nw * 64 + r) * 128;
         const uint8_t *mine = reinterpret_cast<const uint8_t *>(scales + (nw * 64 + r) * PANEL + t % PANEL) + g;
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
@@ -490,7 +493,7 @@ __global__ void __launch_bounds__(512) lvx_fp4_tile_kernel(fp4_args_t p) {
         const bool more = step(j + RING) < steps, more_w = more && odd == (RING == 3);
         if (more) stage_a(j + RING);
         if (more_w) stage_w(j + RING);
-        if (odd && (j + 1) % (PANEL / 2) == 0) {
+        if (odd && (j + 1) % (PANEL / KG) == 0) {
             load_scales(j + 1);
             __syncthreads();
         }
@@ -520,22 +523,27 @@ __global__ void __launch_bounds__(512) lvx_fp4_tile_kernel(fp4_args_t p) {
 
     float row_scale[MBW];
     fp4_row_scales<MODE, MBW>(p, m0 + mw * 16 * MBW + r, row_scale);
-    // each group finishes half of the columns' blocks with the other's sums
+    // each group finishes NB / KG of the columns' blocks with the others' sums, adding in the order of the groups
     f32x4_t *part = reinterpret_cast<f32x4_t *>(lds);
 #pragma unroll
-    for (int b = 0; b < NB / 2; ++b)
+    for (int b = 0; b < NB; ++b)
 #pragma unroll
-        for (int c = 0; c < MBW; ++c) part[((wave * (NB / 2) + b) * MBW + c) * 64 + lane] = kg == 0 ? acc[b + NB / 2][c] : acc[b][c];
+        for (int c = 0; c < MBW; ++c)
+            if (b / (NB / KG) != kg) part[((wave * NB + b) * MBW + c) * 64 + lane] = acc[b][c];
     __syncthreads();
 #pragma unroll
-    for (int b = 0; b < NB / 2; ++b) {
+    for (int b = 0; b < NB; ++b) {
+        if (b / (NB / KG) != kg) continue;
         f32x4_t sum[MBW];
 #pragma unroll
         for (int c = 0; c < MBW; ++c) {
-            const f32x4_t its = part[(((wave ^ 4) * (NB / 2) + b) * MBW + c) * 64 + lane];
-            sum[c] = kg == 0 ? acc[b][c] + its : its + acc[b + NB / 2][c];  // group 0's sum first
+#pragma unroll
+            for (int k = 0; k < KG; ++k) {
+                const f32x4_t its = k == kg ? acc[b][c] : part[(((k * WAVES + in_group) * NB + b) * MBW + c) * 64 + lane];
+                sum[c] = k == 0 ? its : sum[c] + its;
+            }
         }
-        fp4_store<MBW>(p, m0 + mw * 16 * MBW + r, n0 + nw * 64 + 16 * (b + (kg == 0 ? 0 : NB / 2)) + 4 * g, sum, row_scale);
+        fp4_store<MBW>(p, m0 + mw * 16 * MBW + r, n0 + nw * 64 + 16 * b + 4 * g, sum, row_scale);
     }
 }
 
@@ -577,13 +585,21 @@ void launch_resident(const fp4_args_t &p, hipStream_t stream) {
     hipLaunchKernelGGL((lvx_fp4_resident_kernel<MODE, NB>), dim3((p.N + 16 * NB - 1) / (16 * NB)), dim3(64 * waves), operands > sums ? operands : sums, stream, p);
 }
 
-template <int MODE, int MBW, int RING>
+template <int MODE, int MBW, int KG, int RING>
 void launch_tile(const fp4_args_t &p, hipStream_t stream) {
-    constexpr int stages = 2 * RING * 32 * MBW * (MODE == A_BF16 ? 256 : 128) + 4 * 128 * 128, sums = 8 * 2 * MBW * 1024;
-    constexpr int bytes = stages + 128 * PANEL * 4;
-    static_assert(bytes <= 160 * 1024 && sums <= bytes, "LDS");
-    const dim3 grid((p.N + 127) / 128, (p.M + 32 * MBW - 1) / (32 * MBW));
-    hipLaunchKernelGGL((lvx_fp4_tile_kernel<MODE, MBW, RING>), grid, dim3(512), bytes, stream, p);
+    constexpr int cols = 256 / KG, stages = KG * RING * 32 * MBW * (MODE == A_BF16 ? 256 : 128) + KG * 2 * cols * 128, sums = 8 * 4 * MBW * 1024;
+    constexpr int bytes = stages + cols * PANEL * 4;
+    static_assert(bytes <= 160 * 1024 && sums <= bytes && PANEL % (2 * KG) == 0, "LDS");
+    const dim3 grid((p.N + cols - 1) / cols, (p.M + 32 * MBW - 1) / (32 * MBW));
+    hipLaunchKernelGGL((lvx_fp4_tile_kernel<MODE, MBW, KG, RING>), grid, dim3(512), bytes, stream, p);
+}
+
+template <int MODE>
+void launch_tile_8(const fp4_args_t &p, int blocks, bool four, hipStream_t stream) {
+    if (four)
+        blocks == 2 ? launch_tile<MODE, 2, 4, 2>(p, stream) : launch_tile<MODE, 1, 4, 3>(p, stream);
+    else
+        blocks == 3 ? launch_tile<MODE, 3, 2, 3>(p, stream) : blocks == 2 ? launch_tile<MODE, 2, 2, 3>(p, stream) : launch_tile<MODE, 1, 2, 3>(p, stream);
 }
 
 // Few rows.  More columns to a workgroup share the loads of A; that pays where enough workgroups are left (16 8-bit rows x 5120 x 5120: two blocks of
@@ -608,40 +624,23 @@ void linear_few(const fp4_args_t &p, hipStream_t stream) {
         two ? launch_few<MODE, 4, 2, MODE == A_BF16 ? 1 : 2>(p, 4, stream) : launch_few<MODE, 4, 1, MODE == A_BF16 ? 1 : 2>(p, 4, stream);
 }
 
-// Rows of a tile, in blocks of 32: the fewest rounds of the chip, weighed with what a round costs.  A step takes about as long as two blocks even without any (its requests, its
-// weights, its barrier); 5120 channels, one round: 15, 19 and 22 us with 1, 2 and 3 blocks of 8-bit rows, 23 and 29 with 1 and 2 of bf16.
-int tile_blocks(const fp4_args_t &p, int most) {
-    int best = 0;
-    int64_t least = INT64_MAX;
-    for (int mbw = most; mbw >= 1; --mbw) {
-        const int64_t groups = (int64_t)((p.N + 127) / 128) * ((p.M + 32 * mbw - 1) / (32 * mbw));
-        const int64_t cost = (groups + LVX_NUM_CU - 1) / LVX_NUM_CU * (2 + mbw);
-        if (cost < least) least = cost, best = mbw;
-    }
-    return best;
-}
-
 void linear_launch(const fp4_args_t &p, bool a8, hipStream_t stream) {
     // The mixed instruction lines the products of four neighbouring channels up with the largest of them and cuts what lies 12 binary places below its leading bit (measured;
-    // the fours and the steps are added in fp32).  An output in bf16 is rounded at 8 places anyway, and on normal rows the cut is 4e-6 of a sum: it is taken there, for
-    // twice the rate.  Outputs in fp32 get the rows widened to bf16, whose products and sums are fp32's.
-    const bool native = a8 && p.epi != LVX_EPI_RESID_GATE_F32 && p.epi != LVX_EPI_STORE_F32;
-    // Tiles from the product of rows (in blocks of 16) and columns on where they are faster: 96 x 5120 x 5120 15, 22 and 23 us (mixed, widened, bf16) against 24, 24 and 37 of
-    // the few-row kernel, 200 x 1280 x 5120 15, 22 and 23 against 18, 18 and 28, 48 x 5120 x 5120 15, 22 and 23 against 16, 16 and 20.  Rows have to be within reach of their
-    // 32-bit offsets.
-    const int64_t area = (int64_t)((p.M + 15) / 16) * p.N;
-    const bool tiles = p.M > 32 && area >= (a8 && !native ? 30000 : 16000) && p.lda < (1 << 24) && p.ldw < (1 << 24);
-    if (!tiles) {
+    // the fours and the steps are added in fp32).  An output in bf16 is rounded at 8 places anyway, and on normal rows the cut is 4e-6 of a sum: it is taken there for more
+    // than 32 rows, for twice the rate.  Outputs in fp32 get the rows widened to bf16, whose products and sums are fp32's.
+    const int mode = !a8 ? A_BF16 : p.M > 32 && p.epi != LVX_EPI_RESID_GATE_F32 && p.epi != LVX_EPI_STORE_F32 ? A_NATIVE : A_WIDEN;
+    const lvx_fp4_plan_t pl = lvx_fp4_plan(mode, p.M, p.N, p.K);
+    if (pl.blocks == 0 || p.lda >= 1 << 24 || p.ldw >= 1 << 24) {  // tiles reach their rows with 32-bit offsets
         a8 ? linear_few<A_WIDEN>(p, stream) : linear_few<A_BF16>(p, stream);
         return;
     }
-    const int mbw = tile_blocks(p, a8 ? 3 : 2);
-    if (!a8)
-        mbw == 2 ? launch_tile<A_BF16, 2, 2>(p, stream) : launch_tile<A_BF16, 1, 3>(p, stream);
-    else if (native)
-        mbw == 3 ? launch_tile<A_NATIVE, 3, 3>(p, stream) : mbw == 2 ? launch_tile<A_NATIVE, 2, 3>(p, stream) : launch_tile<A_NATIVE, 1, 3>(p, stream);
+    const bool four = pl.groups == 4;
+    if (mode == A_BF16)
+        four ? launch_tile<A_BF16, 1, 4, 2>(p, stream) : pl.blocks == 2 ? launch_tile<A_BF16, 2, 2, 2>(p, stream) : launch_tile<A_BF16, 1, 2, 3>(p, stream);
+    else if (mode == A_NATIVE)
+        launch_tile_8<A_NATIVE>(p, pl.blocks, four, stream);
     else
-        mbw == 3 ? launch_tile<A_WIDEN, 3, 3>(p, stream) : mbw == 2 ? launch_tile<A_WIDEN, 2, 3>(p, stream) : launch_tile<A_WIDEN, 1, 3>(p, stream);
+        launch_tile_8<A_WIDEN>(p, pl.blocks, four, stream);
 }
 
 lvx_status_t linear(const void *a, int64_t lda, const float *row_scales, bool a8, const void *w, int64_t ldw, const void *s, int64_t lds, void *c,

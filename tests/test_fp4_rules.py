@@ -1,0 +1,57 @@
+"""The rule that chooses the kernel and tile of a linear with 4-bit weights (csrc/lvx_fp4_rules.h, plain C++), evaluated on the CPU: the GPU tests' shapes
+take every tile, with whole and ragged rows, columns and channels."""
+import ctypes as C
+import os
+import shutil
+import subprocess
+
+import pytest
+
+import test_gpu_fp4_linear as gpu_tests
+
+CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2512_04677_amd", "csrc")
+SOURCE = r"""
+#include "lvx_fp4_rules.h"
+extern "C" void plan(int mode, int M, int N, int K, int *out) {
+    const lvx_fp4_plan_t p = lvx_fp4_plan(mode, M, N, K);
+    out[0] = p.blocks, out[1] = p.groups;
+}
+"""
+BF16, WIDEN, NATIVE = 0, 1, 2
+
+
+@pytest.fixture(scope="module")
+def plan(tmp_path_factory):
+    cxx = shutil.which("g++")
+    if cxx is None:
+        pytest.skip("g++ not found")
+    d = tmp_path_factory.mktemp("fp4_rules")
+    (d / "rules.cpp").write_text(SOURCE)
+    lib = str(d / "librules.so")
+    r = subprocess.run([cxx, "-O1", "-Wall", "-Werror", "-std=c++17", "-shared", "-fPIC", "-I" + CSRC, str(d / "rules.cpp"), "-o", lib],
+                       capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr[-2000:]
+    so = C.CDLL(lib)
+
+    def f(mode, M, N, K):
+        out = (C.c_int * 2)()
+        so.plan(mode, M, N, K, out)
+        return tuple(out)
+    return f
+
+
+def test_every_tile_is_tested(plan):
+    every = {BF16: {(2, 2), (1, 2), (1, 4)}, WIDEN: {(3, 2), (2, 2), (1, 2), (2, 4), (1, 4)}, NATIVE: {(3, 2), (2, 2), (1, 2), (2, 4), (1, 4)}}
+    shapes = {s[:3] for s in gpu_tests.SHAPES + gpu_tests.TILES + gpu_tests.LONG + gpu_tests.FORMS}
+    for mode, forms in every.items():
+        seen = {plan(mode, *s) for s in shapes} - {(0, 0)}
+        assert seen == forms, (mode, forms - seen)
+        # every tile with a last step of fewer than 128 channels, and with more steps than the scales of one panel
+        assert {plan(mode, *s) for s in gpu_tests.FORMS if s[2] % 128} >= forms
+        assert {plan(mode, *s) for s in gpu_tests.FORMS if s[2] > 48 * 128} >= forms
+
+
+def test_few_rows_and_small_products_take_no_tile(plan):
+    for mode in (BF16, WIDEN, NATIVE):
+        assert plan(mode, 1, 1 << 24, 128) == (0, 0) and plan(mode, 16, 15360, 5120) == (0, 0) and plan(mode, 100, 8, 32) == (0, 0)
+        assert plan(mode, 1 << 20, 1 << 24, (1 << 31) - 32)[0] > 0

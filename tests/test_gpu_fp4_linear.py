@@ -203,3 +203,13 @@ def test_non_finite_weights_and_rows_of_tiles(lvx, a8, f32):
     bad[:, 7] = bad[:, 5000] = True
     bad[33] = True
     assert torch.equal(torch.isnan(out), bad)
+
+
+# every tile (rows, columns, groups over K) in each of its three arithmetics (tests/test_fp4_rules.py holds the rule to that), channels up to more than the scales of one panel
+FORMS = [(m, n, k) for m, n in ((290, 264), (530, 520), (400, 1288), (200, 4104), (530, 2056), (530, 4104)) for k in (160, 6304)]
+
+
+@pytest.mark.parametrize("a8", [False, True])
+@pytest.mark.parametrize("M,N,K", FORMS)
+def test_every_tile(lvx, M, N, K, a8):
+    test_linear(lvx, M, N, K, a8)
