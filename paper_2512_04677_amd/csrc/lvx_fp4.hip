@@ -257,7 +257,7 @@ __global__ void __launch_bounds__(512) lvx_fp4_few_kernel(fp4_args_t p) {
 }
 
 // ---- rows that fit the LDS ----------------------------------------------------------------------------------------------
-// The same for up to sixteen rows that lie in LDS whole (56 KB of them), with the columns' scales beside them, brought there once while the first weights are on their
+// The same for up to sixteen rows that lie in LDS whole, with the columns' scales beside them, brought there once while the first weights are on their
 // way: the loop then requests nothing but weights, two steps ahead of a wave's own.  One row x 15360 x 5120:
 // 9.4 us, 4.4 TB/s.
 template <int MODE, int NB>
@@ -581,7 +581,7 @@ void launch_few(const fp4_args_t &p, int most_waves, hipStream_t stream) {
 template <int MODE, int NB>
 void launch_resident(const fp4_args_t &p, hipStream_t stream) {
     const int steps = (p.K + 127) / 128, rounds = (steps + 7) / 8, waves = (steps + rounds - 1) / rounds;
-    const int operands = p.M * (p.K * (MODE == A_BF16 ? 2 : 1) + 16) + 16 * NB * (((p.K / LVX_FP4_GROUP + 15) & ~15) + 4), sums = waves * NB * 1024;
+    const int operands = (int)lvx_fp4_resident_bytes(MODE == A_BF16 ? 2 : 1, p.M, p.K, NB), sums = waves * NB * 1024;
     hipLaunchKernelGGL((lvx_fp4_resident_kernel<MODE, NB>), dim3((p.N + 16 * NB - 1) / (16 * NB)), dim3(64 * waves), operands > sums ? operands : sums, stream, p);
 }
 
@@ -606,10 +606,9 @@ void launch_tile_8(const fp4_args_t &p, int blocks, bool four, hipStream_t strea
 // columns are fastest, 8.4 us; 16 bf16 rows x 13824 x 5120: 14.3 with four, 17.5 with two; 1280 columns: one).
 template <int MODE>
 void linear_few(const fp4_args_t &p, hipStream_t stream) {
-    // Rows that fit the LDS beside others' (two workgroups a unit at least) and are long enough to pay for the way there: one row x 15360 x 5120 9.5 us against 12.0, 4 rows 10.9 against
-    // 13.1, 4 8-bit rows x 5120 x 13824 12.4 against 13.8; but 8 bf16 rows of 5120 (82 KB) 10.2 against 8.9, one row x 1280 x 1280 3.9 against 3.2.
-    if (p.M <= 16 && p.K >= 4096 && (int64_t)p.M * p.K * (MODE == A_BF16 ? 2 : 1) <= 56 * 1024) {
-        p.N >= 8192 ? launch_resident<MODE, 2>(p, stream) : launch_resident<MODE, 1>(p, stream);
+    const int nb = lvx_fp4_resident(MODE == A_BF16 ? 2 : 1, p.M, p.N, p.K);
+    if (nb != 0) {
+        nb == 4 ? launch_resident<MODE, 4>(p, stream) : nb == 2 ? launch_resident<MODE, 2>(p, stream) : launch_resident<MODE, 1>(p, stream);
         return;
     }
     const int blocks = (p.M + 15) / 16, tiles = (blocks + 3) / 4, mb = (blocks + tiles - 1) / tiles;

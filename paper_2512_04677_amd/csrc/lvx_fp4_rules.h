@@ -35,3 +35,23 @@ static inline lvx_fp4_plan_t lvx_fp4_plan(int mode, int M, int N, int K) {
     }
     return best;
 }
+
+// Rows that lie in LDS whole, of K values of `bytes` bytes, beside the scales of 16 nb columns.
+static inline int64_t lvx_fp4_resident_bytes(int bytes, int M, int K, int nb) { return (int64_t)M * ((int64_t)K * bytes + 16) + 16 * nb * (((K / 32 + 15) & ~15) + 4); }
+
+// Blocks of 16 columns of such a workgroup, 0 where the rows are better loaded as they are multiplied.  Rows have to be long enough to pay for the way to LDS (1 x 1280 x 1280
+// 3.9 us against 3.2).  The fewest columns with which all workgroups stay at once, two a compute unit or, where there are few enough, one of all its LDS: one row x 5120 x 5120
+// 6.7 us against 8.2, 12 bf16 rows 9.8 (two blocks, one workgroup a unit) against 10.4, 14 8-bit rows x 13824 x 5120 13.0 against 13.7, 12 x 27648 x 5120 22.3 (four blocks)
+// against 25.3; but 12 bf16 rows x 13824 x 5120 16.2 in four blocks with a unit's LDS each against 15.0.  Columns for fewer than half the units leave the rows' way bare: 14 8-bit
+// rows x 1280 x 5120 6.7 against 5.9.  Where all columns take several rounds anyway, many small workgroups hide each other's starts: 1 x 27648 x 5120 17.8 in single blocks, 19.9
+// in four.
+static inline int lvx_fp4_resident(int bytes, int M, int N, int K) {
+    if (M > 16 || K < 4096) return 0;
+    const int64_t all = 160 * 1024, one = ((int64_t)N + 15) / 16, two = ((int64_t)N + 31) / 32;
+    const int64_t need = lvx_fp4_resident_bytes(bytes, M, K, 1), need2 = lvx_fp4_resident_bytes(bytes, M, K, 2);
+    if (one < 128) return (int64_t)M * K * bytes <= 56 * 1024 && need <= all ? 1 : 0;
+    if (one > 1024 && need <= all / 6) return 1;
+    if ((one <= 512 && need <= all / 2) || (one <= 256 && need <= all)) return 1;
+    if ((two <= 512 && need2 <= all / 2) || (two <= 256 && need2 <= all)) return 2;
+    return lvx_fp4_resident_bytes(bytes, M, K, 4) <= all / 2 ? 4 : 0;
+}

@@ -16,6 +16,8 @@ extern "C" void plan(int mode, int M, int N, int K, int *out) {
     const lvx_fp4_plan_t p = lvx_fp4_plan(mode, M, N, K);
     out[0] = p.blocks, out[1] = p.groups;
 }
+extern "C" int resident(int bytes, int M, int N, int K) { return lvx_fp4_resident(bytes, M, N, K); }
+extern "C" long long resident_bytes(int bytes, int M, int K, int nb) { return lvx_fp4_resident_bytes(bytes, M, K, nb); }
 """
 BF16, WIDEN, NATIVE = 0, 1, 2
 
@@ -37,6 +39,8 @@ def plan(tmp_path_factory):
         out = (C.c_int * 2)()
         so.plan(mode, M, N, K, out)
         return tuple(out)
+    so.resident_bytes.restype = C.c_longlong
+    f.so = so
     return f
 
 
@@ -55,3 +59,17 @@ def test_few_rows_and_small_products_take_no_tile(plan):
     for mode in (BF16, WIDEN, NATIVE):
         assert plan(mode, 1, 1 << 24, 128) == (0, 0) and plan(mode, 16, 15360, 5120) == (0, 0) and plan(mode, 100, 8, 32) == (0, 0)
         assert plan(mode, 1 << 20, 1 << 24, (1 << 31) - 32)[0] > 0
+
+
+def test_rows_in_lds(plan):
+    so = plan.so
+    for (M, N, K), nb in gpu_tests.IN_LDS.items():
+        assert (so.resident(2, M, N, K), so.resident(1, M, N, K)) == nb, (M, N, K)
+    assert {n for pair in gpu_tests.IN_LDS.values() for n in pair} == {0, 1, 2, 4}
+    for bytes_ in (1, 2):
+        for M in range(1, 18):
+            for K in list(range(4000 // 32 * 32, 200000, 1184)) + [(1 << 31) - 32]:
+                for N in (8, 1280, 2568, 5120, 8200, 13824, 27648, 1 << 24):
+                    nb = so.resident(bytes_, M, N, K)
+                    # never more than a compute unit's LDS
+                    assert nb == 0 or (M <= 16 and so.resident_bytes(bytes_, M, K, nb) <= 160 * 1024)

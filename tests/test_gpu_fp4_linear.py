@@ -213,3 +213,14 @@ FORMS = [(m, n, k) for m, n in ((290, 264), (530, 520), (400, 1288), (200, 4104)
 @pytest.mark.parametrize("M,N,K", FORMS)
 def test_every_tile(lvx, M, N, K, a8):
     test_linear(lvx, M, N, K, a8)
+
+
+# rows that lie in LDS whole: blocks of 16 columns to a workgroup for (bf16, 8-bit) rows, 0 for the other kernel
+IN_LDS = {(1, 264, 4128): (1, 1), (5, 5128, 5120): (1, 1), (9, 5128, 5120): (2, 1), (16, 2056, 6304): (0, 1), (11, 2056, 6304): (1, 1), (13, 13832, 5120): (0, 2),
+          (3, 16456, 4128): (1, 1), (6, 16456, 5152): (4, 4), (16, 5128, 5120): (0, 2), (5, 5128, 13824): (2, 1), (14, 264, 5120): (0, 0)}
+
+
+@pytest.mark.parametrize("a8", [False, True])
+@pytest.mark.parametrize("M,N,K", list(IN_LDS))
+def test_rows_in_lds(lvx, M, N, K, a8):
+    test_linear(lvx, M, N, K, a8)
