@@ -325,9 +325,10 @@ __global__ void __launch_bounds__(64 * WR * WK, 2) lvx_kv4_attention_kernel(attn
 
     f32x4_t o[RB][CB];
     float ref[RB], sum[RB];
+    bool unset[RB];  // a row of the block has no reference yet and sees keys from here on
 #pragma unroll
     for (int b = 0; b < RB; ++b) {
-        ref[b] = -INFINITY, sum[b] = 0;
+        ref[b] = -INFINITY, sum[b] = 0, unset[b] = true;
 #pragma unroll
         for (int c = 0; c < CB; ++c) o[b][c] = {0, 0, 0, 0};
     }
@@ -411,9 +412,9 @@ __global__ void __launch_bounds__(64 * WR * WK, 2) lvx_kv4_attention_kernel(attn
             // The reference that is subtracted only has to keep the powers inside fp32.  With the running maximum the largest probability is 1 and its rounding exact, which
             // peaked rows notice (errors of 1.7e-3 against 2.1e-3 with a reference that lags by up to 2^20): where the cache's bytes bound the kernel, that is what it is.
             // Where the vector unit does (one wave per tile of keys), it is the first tile's maximum, and a tile whose powers reach 2^4 of it moves it (1.9e-3).
-            // A row without a reference sees none of the tiles so far, nor any later one (a row sees a prefix of the keys).
+            // A row whose scores so far are all -infinity takes its reference from the next tile, above zero or below.
             constexpr bool RUNNING = WK > 1;
-            bool move = t == t0 + wk;
+            bool move = unset[b];
             float m = -INFINITY;
             auto maximum = [&]() {
 #pragma unroll
@@ -435,6 +436,7 @@ __global__ void __launch_bounds__(64 * WR * WK, 2) lvx_kv4_attention_kernel(attn
                 base = next == -INFINITY ? 0.f : next;
                 const float shrink = __builtin_amdgcn_exp2f(ref[b] - base);
                 ref[b] = next;
+                unset[b] = __any(next == -INFINITY && seen[b] > TILE * (t + 1));
                 exponents();
                 sum[b] *= shrink;
 #pragma unroll

@@ -304,3 +304,24 @@ def test_every_form(lvx, D, S_, KV, group, n, L, rows_, splits):
             tol = 2.0 ** -8 * np.abs(ref) + (2.0 ** -8 + 2.0 ** -16 + 2 * (D + 4) * 2.0 ** -24 * size[..., None]) * spread
             err = np.abs(S.to_f64(out[sel]).reshape(ref.shape) - ref)
             assert np.all(err <= tol), (s, causal, float((err - tol).max()))
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("S_,KV,group,n,L,rows_,splits", FORMS)
+def test_keys_whose_scores_overflow(lvx, D, S_, KV, group, n, L, rows_, splits):
+    """The first keys' scores pass fp32 below (-infinity: probability zero), those behind them are finite and negative: they alone make the output."""
+    H, hidden = KV * group, L // 2 // 64 * 64 + 10
+    cache = lvx.KV4Cache(lvx.kv4_desc(1, S_, KV, D, L), DEV)
+    q = torch.full((S_ * n, H * D), 2.0 ** 60, dtype=torch.bfloat16, device=DEV)
+    k = (-(2.0 ** -60) * (1 + 0.3 * rows(S_ * L, KV * D, "over_k", L).float().tanh())).to(torch.bfloat16).view(S_, L, KV * D)
+    k[:, :hidden] = -(2.0 ** 70)
+    v = rows(S_ * L, KV * D, "over_v", L)
+    counts = i32([L] * S_)
+    lvx.lvx_kv4_append(cache, 0, k.flatten(0, 1), v, counts, max_tokens=L)
+    ws = torch.empty(lvx.lvx_kv4_attention_workspace_bytes(cache, H, n), dtype=torch.uint8, device=DEV)
+    out = torch.empty_like(q)
+    lvx.lvx_kv4_attention(cache, 0, q, H, 0.1, counts, out, ws, max_tokens=n, causal=False)
+    dk, dv = decoded(k[0, hidden:], KV, D), decoded_v(v[hidden:L], KV, D)
+    ref, spread, size = O.attention(S.to_f64(q[:1]).reshape(1, H, D), dk, dv, 0.1, [L - hidden])
+    tol = 2.0 ** -8 * np.abs(ref) + (2.0 ** -8 + 2.0 ** -16 + 2 * (D + 4) * 2.0 ** -24 * size[..., None]) * spread
+    assert np.all(np.abs(S.to_f64(out[:n]).reshape(n, H, D) - ref) <= tol)
