@@ -306,14 +306,18 @@ __global__ void __launch_bounds__(64 * WR * WK, 2) lvx_kv4_attention_kernel(attn
 #pragma unroll
     for (int b = 0; b < RB; ++b) {
         const int row = row0 + 16 * b + r;
-        const int i = row < n_rows ? row / p.group : sp.n - 1;
-        const int head_of = head * p.group + (row < n_rows ? row % p.group : 0);
-        seen[b] = row < n_rows ? keys_seen(sp, i, p.causal, p.max_keys) : 0;
-        const uint4 *src = reinterpret_cast<const uint4 *>(p.q + (int64_t)(sp.first + i) * p.ld_q + head_of * D + (D / 4) * g);
+        seen[b] = 0;
 #pragma unroll
-        for (int j = 0; j < KS; ++j) {
-            const uint4 v = src[j];
-            q[b][j] = *reinterpret_cast<const bf16x8_t *>(&v);
+        for (int j = 0; j < KS; ++j) q[b][j] = bf16x8_t{};
+        if (row < n_rows) {  // rows behind the last one read nothing: every other row may be another workgroup's, which stores its output over it
+            const int i = row / p.group;
+            seen[b] = keys_seen(sp, i, p.causal, p.max_keys);
+            const uint4 *src = reinterpret_cast<const uint4 *>(p.q + (int64_t)(sp.first + i) * p.ld_q + (head * p.group + row % p.group) * D + (D / 4) * g);
+#pragma unroll
+            for (int j = 0; j < KS; ++j) {
+                const uint4 v = src[j];
+                q[b][j] = *reinterpret_cast<const bf16x8_t *>(&v);
+            }
         }
     }
     // the keys that any of the workgroup's rows sees, and those that all of this wave's rows see
@@ -328,7 +332,8 @@ __global__ void __launch_bounds__(64 * WR * WK, 2) lvx_kv4_attention_kernel(attn
     bool unset[RB];  // a row of the block has no reference yet and sees keys from here on
 #pragma unroll
     for (int b = 0; b < RB; ++b) {
-        ref[b] = -INFINITY, sum[b] = 0, unset[b] = true;
+        ref[b] = row0 + 16 * b + r < n_rows ? -INFINITY : INFINITY;  // a row behind the last one: every power is zero, and it has no say in the votes
+        sum[b] = 0, unset[b] = true;
 #pragma unroll
         for (int c = 0; c < CB; ++c) o[b][c] = {0, 0, 0, 0};
     }

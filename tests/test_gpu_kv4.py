@@ -325,3 +325,25 @@ def test_keys_whose_scores_overflow(lvx, D, S_, KV, group, n, L, rows_, splits):
     ref, spread, size = O.attention(S.to_f64(q[:1]).reshape(1, H, D), dk, dv, 0.1, [L - hidden])
     tol = 2.0 ** -8 * np.abs(ref) + (2.0 ** -8 + 2.0 ** -16 + 2 * (D + 4) * 2.0 ** -24 * size[..., None]) * spread
     assert np.all(np.abs(S.to_f64(out[:n]).reshape(n, H, D) - ref) <= tol)
+
+
+# sequences, kv heads, heads of a group, tokens, keys; rows of a workgroup: in the last block of rows fewer than a token's heads are left
+IN_PLACE = [(1, 6, 5, 141, 200, 16), (1, 2, 3, 715, 3000, 32), (4, 6, 5, 205, 300, 64), (1, 8, 5, 1549, 1560, 64), (16, 8, 5, 77, 130, 128), (16, 6, 5, 77, 130, 128)]
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("S_,KV,group,n,L,rows_", IN_PLACE)
+def test_in_place(lvx, D, S_, KV, group, n, L, rows_):
+    """Outputs over the queries are the bits of outputs elsewhere: no workgroup reads a query that another may have stored over."""
+    tag, H = "place%d_%d_%d" % (KV, n, L), KV * group
+    cache = lvx.KV4Cache(lvx.kv4_desc(1, S_, KV, D, L), DEV)
+    counts = i32([L - s for s in range(S_)])
+    lvx.lvx_kv4_append(cache, 0, rows(S_ * L, KV * D, tag, "k"), rows(S_ * L, KV * D, tag, "v"), i32([L] * S_), max_tokens=L)
+    q = rows(S_ * n, H * D, tag, "q")
+    ws = torch.empty(lvx.lvx_kv4_attention_workspace_bytes(cache, H, n), dtype=torch.uint8, device=DEV)
+    out = torch.empty_like(q)
+    lvx.lvx_kv4_attention(cache, 0, q, H, 1.0, counts, out, ws, max_tokens=n)
+    for _ in range(4):
+        both = q.clone()
+        lvx.lvx_kv4_attention(cache, 0, both, H, 1.0, counts, both, ws, max_tokens=n)
+        assert torch.equal(both, out)

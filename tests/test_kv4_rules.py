@@ -65,3 +65,9 @@ def test_plans_stay_inside_the_workspace(rules):
         assert 1 <= splits <= min(64, -(-L // 64)) and (splits == 1 or splits * row_tiles * KV * S <= 512)
         if splits > 1:
             assert splits * n * S * KV * group <= rules[1](S, L, KV * group, n) and n * KV * group < 1 << 24
+
+
+def test_forms_of_the_in_place_tests(rules):
+    for S, KV, group, n, L, form in gpu_tests.IN_PLACE:
+        assert rules[0](S, KV, L, KV * group, n)[0] == form and 0 < n * group % min(form, 32) < group
+    assert {f for *_, f in gpu_tests.IN_PLACE} == {16, 32, 64, 128}
