@@ -13,6 +13,7 @@ _lib = None
 
 LVX_MAX_SLOTS = 16
 EPI_STORE, EPI_GELU_TANH, EPI_RESID_GATE, EPI_RESID_GATE_F32, EPI_BIAS, EPI_BIAS_SILU, EPI_STORE_F32 = 0, 1, 2, 3, 4, 5, 6
+EPI_MIXED_8X4 = 16  # a flag: lvx_linear_fp8_fp4's bf16 epilogues take it
 STATUS_NAMES = {0: "LVX_OK", 1: "LVX_ERR_INVALID_ARG", 2: "LVX_ERR_SHAPE", 3: "LVX_ERR_STATE", 4: "LVX_ERR_UNSUPPORTED",
                 5: "LVX_ERR_HIP"}
 
@@ -404,7 +405,7 @@ def lvx_linear_fp4(a, wq, w_scales, c, epi=EPI_STORE, resid=None, gate=None):
 
 
 def lvx_linear_fp8_fp4(aq, row_scales, wq, w_scales, c, epi=EPI_STORE, resid=None, gate=None):
-    """The same for E4M3 rows (uint8 [M][K]) with one fp32 scale each."""
+    """The same for E4M3 rows (uint8 [M][K]) with one fp32 scale each.  epi | EPI_MIXED_8X4 allows many rows the faster 8 x 4-bit products, which cut the small ones of four."""
     M, K = aq.shape
     if M:
         _check(load().lvx_linear_fp8_fp4(aq.data_ptr(), aq.stride(0), row_scales.data_ptr(), wq.data_ptr(), wq.stride(0), w_scales.data_ptr(),

@@ -623,11 +623,11 @@ void linear_few(const fp4_args_t &p, hipStream_t stream) {
         two ? launch_few<MODE, 4, 2, MODE == A_BF16 ? 1 : 2>(p, 4, stream) : launch_few<MODE, 4, 1, MODE == A_BF16 ? 1 : 2>(p, 4, stream);
 }
 
-void linear_launch(const fp4_args_t &p, bool a8, hipStream_t stream) {
-    // The mixed instruction lines the products of four neighbouring channels up with the largest of them and cuts what lies 12 binary places below its leading bit (measured;
-    // the fours and the steps are added in fp32).  An output in bf16 is rounded at 8 places anyway, and on normal rows the cut is 4e-6 of a sum: it is taken there for more
-    // than 32 rows, for twice the rate.  Outputs in fp32 get the rows widened to bf16, whose products and sums are fp32's.
-    const int mode = !a8 ? A_BF16 : p.M > 32 && p.epi != LVX_EPI_RESID_GATE_F32 && p.epi != LVX_EPI_STORE_F32 ? A_NATIVE : A_WIDEN;
+void linear_launch(const fp4_args_t &p, bool a8, bool mixed, hipStream_t stream) {
+    // 8-bit rows are widened to bf16, whose products with the weights are exact, and summed in fp32.  A caller may ask for the mixed instruction, E4M3 by E2M1 at twice the rate
+    // (544 x 5120 x 13824: 51 us against 84): it lines the products of four neighbouring channels up with the largest of them and cuts what lies 12 binary places below
+    // its leading bit (measured; the fours and the steps are added in fp32), on normal rows 4e-6 of a sum.  Up to 32 rows are bound by the weights and are widened all the same.
+    const int mode = !a8 ? A_BF16 : mixed && p.M > 32 ? A_NATIVE : A_WIDEN;
     const lvx_fp4_plan_t pl = lvx_fp4_plan(mode, p.M, p.N, p.K);
     if (pl.blocks == 0 || p.lda >= 1 << 24 || p.ldw >= 1 << 24) {  // tiles reach their rows with 32-bit offsets
         a8 ? linear_few<A_WIDEN>(p, stream) : linear_few<A_BF16>(p, stream);
@@ -655,8 +655,11 @@ lvx_status_t linear(const void *a, int64_t lda, const float *row_scales, bool a8
     LVX_REQUIRE(lda >= K && lda % (a8 ? 16 : 8) == 0 && ldw >= K / 2 && ldw % 16 == 0 && lds >= K / LVX_FP4_GROUP && ldc >= N && ldc % 8 == 0,
                 LVX_ERR_SHAPE, "bad leading dimension");
     LVX_REQUIRE(M <= 1 << 20, LVX_ERR_SHAPE, "M %d is more than 2^20 rows", M);
+    const bool mixed = a8 && ((int)epi & LVX_EPI_MIXED_8X4) != 0;
+    if (mixed) epi = (lvx_epilogue_t)((int)epi & ~LVX_EPI_MIXED_8X4);
     LVX_REQUIRE(epi == LVX_EPI_STORE || epi == LVX_EPI_GELU_TANH || epi == LVX_EPI_RESID_GATE || epi == LVX_EPI_RESID_GATE_F32 || epi == LVX_EPI_STORE_F32,
                 LVX_ERR_INVALID_ARG, "unknown epilogue %d", (int)epi);
+    LVX_REQUIRE(!mixed || (epi != LVX_EPI_RESID_GATE_F32 && epi != LVX_EPI_STORE_F32), LVX_ERR_INVALID_ARG, "mixed products are for bf16 outputs, not epilogue %d", (int)epi);
     if (epi == LVX_EPI_RESID_GATE || epi == LVX_EPI_RESID_GATE_F32) {
         LVX_REQUIRE(resid != nullptr, LVX_ERR_INVALID_ARG, "residual epilogue needs a residual pointer");
         LVX_REQUIRE(ldr >= N && ldr % 8 == 0, LVX_ERR_SHAPE, "bad residual leading dimension");
@@ -671,7 +674,7 @@ lvx_status_t linear(const void *a, int64_t lda, const float *row_scales, bool a8
     p.R = resid, p.ldr = ldr;
     p.gate = gate;
     p.M = M, p.N = N, p.K = K, p.epi = (int)epi;
-    linear_launch(p, a8, stream);
+    linear_launch(p, a8, mixed, stream);
     LVX_CHECK_HIP(hipGetLastError());
     return LVX_OK;
 }

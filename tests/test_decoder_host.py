@@ -168,3 +168,15 @@ def test_python_binding_refuses_what_would_fault():
         lvx.lvx_kv4_gather(Stub, 0, good, out, out[:, :2])
     lvx.lvx_kv4_gather(Stub, 0, good, out[:, :0], out[:, :0])
     lvx.lvx_rmsnorm_residual(x[:0], None, None, 1e-6, c[:0])
+
+
+def test_mixed_products_are_for_8bit_rows_and_bf16_outputs():
+    lib, flag = lvx.load(), lvx.EPI_MIXED_8X4
+    a16 = (P, 64, P, 32, P, 2, P, 16, 0, 16, 64)
+    a8 = (P, 64, P, P, 32, P, 2, P, 16, 0, 16, 64)
+    for epi in (lvx.EPI_STORE, lvx.EPI_GELU_TANH, lvx.EPI_RESID_GATE):
+        assert lib.lvx_linear_fp8_fp4(*a8, epi | flag, P, 16, None, None) == 0
+        assert lib.lvx_linear_fp4(*a16, epi | flag, P, 16, None, None) == 1
+    for epi in (lvx.EPI_RESID_GATE_F32, lvx.EPI_STORE_F32, lvx.EPI_BIAS, lvx.EPI_BIAS_SILU, 7, 16):
+        assert lib.lvx_linear_fp8_fp4(*a8, epi | flag, P, 16, None, None) == (0 if epi == 16 else 1)
+    assert lib.lvx_linear(P, 64, P, 64, P, 16, 8, 16, 64, flag, None, 0, None, None) == 1

@@ -224,3 +224,78 @@ IN_LDS = {(1, 264, 4128): (1, 1), (5, 5128, 5120): (1, 1), (9, 5128, 5120): (2, 
 @pytest.mark.parametrize("M,N,K", list(IN_LDS))
 def test_rows_in_lds(lvx, M, N, K, a8):
     test_linear(lvx, M, N, K, a8)
+
+
+def unequal(M, N, K):
+    """E4M3 codes that differ by up to 2^17 within a four, with pairs that cancel, and weights that are equal on those pairs."""
+    gen = lambda seed: torch.Generator(device=DEV).manual_seed(seed)
+    c = torch.randint(0, 256, (M, K), device=DEV, generator=gen(21)).to(torch.uint8)
+    c[(c & 127) == 127] = 0
+    c[:, 1::16] = c[:, 0::16] ^ 128
+    q = torch.randint(0, 256, (N, K // 2), device=DEV, generator=gen(22)).to(torch.uint8)
+    q[:, 0::8] = (q[:, 0::8] & 15) * 17
+    s = torch.full((N, K // 32), 127, dtype=torch.uint8, device=DEV)
+    return c, torch.ones(M, device=DEV), q, s, e4m3_decode(c.cpu().numpy()), O.e2m1_value(unpack(q))
+
+
+@pytest.mark.parametrize("M,N,K", [(33, 5120, 128), (256, 5120, 128), (530, 520, 160), (96, 4104, 6304)])
+def test_many_8bit_rows_are_summed_in_fp32(lvx, M, N, K):
+    """Terms far below their neighbours keep their bits, with bf16 outputs as with fp32 ones: those are the same sums, rounded."""
+    c, one, q, s, a, w = unequal(M, N, K)
+    ref, off = a @ w.T, (K + 8) * 2.0 ** -24 * (np.abs(a) @ np.abs(w).T)
+    out, o32 = torch.empty(M, N, dtype=torch.bfloat16, device=DEV), torch.empty(M, N, device=DEV)
+    lvx.lvx_linear_fp8_fp4(c, one, q, s, out)
+    lvx.lvx_linear_fp8_fp4(c, one, q, s, o32, lvx.EPI_STORE_F32)
+    assert np.all(np.abs(S.to_f64(out) - ref) <= 2.0 ** -8 * np.abs(ref) + off) and np.all(np.abs(S.to_f64(o32) - ref) <= off)
+    assert torch.equal(out, o32.to(torch.bfloat16))
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 8200, 5120), (32, 264, 512), (33, 136, 128), (70, 4104, 6304)] + FORMS)
+def test_mixed_products_on_request(lvx, M, N, K):
+    """With the flag: within the bound of those products in every tile, the same bits from the same call, and no other bits where the rows are few."""
+    call, ref, off, cut = products(lvx, M, N, K, True, "mix")
+    out = torch.full((M + 1, N + 8), 7.0, dtype=torch.bfloat16, device=DEV)
+    call(out[:M, :N], lvx.EPI_STORE | lvx.EPI_MIXED_8X4)
+    assert np.all(np.abs(S.to_f64(out[:M, :N]) - ref) <= 2.0 ** -8 * np.abs(ref) + 2 * (off + cut))
+    assert bool((out[M:] == 7).all()) and bool((out[:, N:] == 7).all())
+    again = torch.empty(M, N, dtype=torch.bfloat16, device=DEV)
+    call(again, lvx.EPI_STORE | lvx.EPI_MIXED_8X4)
+    assert torch.equal(again, out[:M, :N])
+    if M <= 32:
+        call(again)
+        assert torch.equal(again, out[:M, :N])
+    r, g = S.randn_bf16((M, N), S.seed_of("mix_r", M, N), 2.0, device=DEV), S.randn_f32((N,), S.seed_of("mix_g", N), 1.0, device=DEV)
+    gg = S.to_f64(g)
+    want = S.to_f64(r) + gg * ref
+    c = r.clone()
+    call(c, lvx.EPI_RESID_GATE | lvx.EPI_MIXED_8X4, resid=c, gate=g)
+    assert np.all(np.abs(S.to_f64(c) - want) <= 2.0 ** -8 * np.abs(want) + 2 * (off * np.abs(gg) + 2.0 ** -24 * np.abs(gg * ref)) + 2 * cut * np.abs(gg))
+    call(c, lvx.EPI_GELU_TANH | lvx.EPI_MIXED_8X4)
+    want = gelu_tanh(ref)
+    assert np.all(np.abs(S.to_f64(c) - want) <= 2.0 ** -8 * np.abs(want) + 2 * (off + cut) + 2.0 ** -18 * np.abs(ref))
+
+
+def test_mixed_products_lose_no_more_than_their_bound(lvx):
+    c, one, q, s, a, w = unequal(256, 5120, 128)
+    ref, off, cut = a @ w.T, (128 + 8) * 2.0 ** -24 * (np.abs(a) @ np.abs(w).T), mixed(a, w)
+    out = torch.empty(256, 5120, dtype=torch.bfloat16, device=DEV)
+    lvx.lvx_linear_fp8_fp4(c, one, q, s, out, lvx.EPI_STORE | lvx.EPI_MIXED_8X4)
+    err = np.abs(S.to_f64(out) - ref) - 2.0 ** -8 * np.abs(ref)
+    print("beyond the output's rounding: %.3f of the bound at most" % (err / cut).max(), flush=True)
+    assert np.all(err <= cut + off)
+
+
+def test_mixed_products_keep_what_is_not_finite(lvx):
+    M, N, K = 48, 5464, 288
+    q, s = lvx.lvx_fp4_quantize(S.randn_bf16((N, K), S.seed_of("nfm", "w"), 1.0, device=DEV))
+    s = s.clone()
+    s[7, 8], s[5000, 0] = 255, 255
+    a = torch.full((M, K + 32), 0x7f, dtype=torch.uint8, device=DEV)
+    a[:, :K] = S.randn_f32((M, K), S.seed_of("nfm", "a"), 60.0, device=DEV).to(torch.float8_e4m3fn).view(torch.uint8)
+    a[33, 280] = 0x7f
+    out = torch.empty(M, N, dtype=torch.bfloat16, device=DEV)
+    lvx.lvx_linear_fp8_fp4(a[:, :K], torch.ones(M, device=DEV), q, s, out, lvx.EPI_STORE | lvx.EPI_MIXED_8X4)
+    bad = torch.zeros(M, N, dtype=torch.bool, device=DEV)
+    bad[:, 7] = bad[:, 5000] = True
+    bad[33] = True
+    assert torch.equal(torch.isnan(out), bad)
