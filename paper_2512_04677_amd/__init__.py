@@ -164,13 +164,53 @@ def _stream():
     return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
-def _stream_of(t):
-    """The same for a launch that works on t, which has to lie on that device: another device's (or the host's) address would fault the kernel."""
+def _here():
+    """The current device and its current HIP stream."""
     import torch
+    device = torch._C._cuda_getDevice()
+    return device, torch._C._cuda_getCurrentRawStream(device)
+
+
+def _here_with(t, what):
+    """The same for a call that works on t, which has to lie on that device: another device's (or the host's) address would fault the kernel."""
     d = t.get_device()
-    if d < 0 or d != torch._C._cuda_getDevice():
-        raise LvxError(1, f"a tensor lies on {t.device}, not on the current device")
-    return torch._C._cuda_getCurrentRawStream(d)
+    if d >= 0:
+        here = _here()
+        if here[0] == d:
+            return here
+    raise LvxError(1, f"{what} lies on {t.device}, not on the current device")
+
+
+def _matrix(t, what, dtype, rows, cols, device):
+    """Address and row stride of a tensor that the library takes as [rows][cols] of dtype: what the kernel would read or write has to be there."""
+    try:
+        r, c = t.shape
+        ld, step = t.stride()
+        if r >= rows and c >= cols and t.dtype is dtype and t.get_device() == device and (step == 1 or cols < 2):
+            return t.data_ptr(), ld
+    except ValueError:  # not two dimensions
+        pass
+    if t.get_device() != device:
+        raise LvxError(1, f"{what} lies on {t.device}, not on the current device")
+    if t.dtype is not dtype:
+        raise LvxError(1, f"{what} is {t.dtype}, not {dtype}")
+    raise LvxError(2, f"{what} of shape {tuple(t.shape)} and strides {t.stride()} does not hold {rows} rows of {cols} neighbouring elements")
+
+
+def _vector(t, what, n, device):
+    """Address of n fp32 in a row (None: NULL)."""
+    if t is None:
+        return None
+    import torch
+    if t.get_device() == device and t.dtype is torch.float32 and t.numel() >= n and t.is_contiguous():
+        return t.data_ptr()
+    raise LvxError(1, f"{what} is a contiguous float32 tensor of at least {n} elements on the current device")
+
+
+def _e4m3(t):
+    """The dtype of E4M3 codes: uint8, or torch's own."""
+    import torch
+    return torch.float8_e4m3fn if t.dtype is torch.float8_e4m3fn else torch.uint8
 
 
 def _check_i32(t, n, like):
@@ -356,61 +396,90 @@ def lvx_layernorm_modulate(x, shift, scale, eps, u):
                                          _ptr(u), u.stride(0), _stream()))
 
 
-def _norm_args(x, resid, gain, eps, sum_out):
+def _norm_args(x, resid, gain, eps, sum_out, y, y_type):
+    """The norms' arguments up to y, the device and the stream; no rows: None."""
     import torch
-    n, d = (resid if x is None else x).shape
-    return (_ptr(x), 0 if x is None else x.stride(0), _ptr(resid), 0 if resid is None else resid.stride(0),
-            0 if resid is None or resid.dtype != torch.float32 else 1, _ptr(gain), eps, n, d, _ptr(sum_out), 0 if sum_out is None else sum_out.stride(0))
+    like = resid if x is None else x
+    if like is None:
+        raise LvxError(1, "x and the residual are both None")
+    if sum_out is not None and (resid is None or sum_out.dtype != resid.dtype):
+        raise LvxError(1, "the sum has the residual's dtype")
+    shape = like.shape
+    n, d = shape
+    if n == 0:
+        return None
+    device, stream = _here_with(y, "y")
+    x, ldx = (None, 0) if x is None else _matrix(x, "x", torch.bfloat16, n, d, device)
+    r, ldr, s, ld_sum, f32 = None, 0, None, 0, 0
+    if resid is not None:
+        f32 = 1 if resid.dtype is torch.float32 else 0
+        if resid is not like and resid.shape != shape:
+            raise LvxError(2, f"x and the residual are of shapes {tuple(shape)} and {tuple(resid.shape)}")
+        r, ldr = _matrix(resid, "the residual", torch.float32 if f32 else torch.bfloat16, n, d, device)
+        if sum_out is not None:
+            s, ld_sum = _matrix(sum_out, "the sum", torch.float32 if f32 else torch.bfloat16, n, d, device)
+    return (x, ldx, r, ldr, f32, _vector(gain, "gain", d, device), eps, n, d, s, ld_sum, *_matrix(y, "y", y_type, n, d, device)), device, stream
 
 
 def lvx_rmsnorm_residual(x, resid, gain, eps, y, sum_out=None):
     """y = RMSNorm(x + resid) * gain in bf16; sum_out (the residual's dtype) receives x + resid.  x or resid may be None.  No rows: nothing is done."""
-    _check_like(resid, sum_out)
-    a = _norm_args(x, resid, gain, eps, sum_out)
-    if a[7]:
-        _check(load().lvx_rmsnorm_residual(*a, y.data_ptr(), y.stride(0), _stream_of(y)))
+    import torch
+    found = _norm_args(x, resid, gain, eps, sum_out, y, torch.bfloat16)
+    if found is not None:
+        a, device, stream = found
+        _check(load().lvx_rmsnorm_residual(*a, stream))
 
 
 def lvx_rmsnorm_residual_fp8(x, resid, gain, eps, q, row_scales, sum_out=None):
     """The same with y as E4M3 codes (uint8 [n][>= d]) and one fp32 scale a row."""
-    _check_like(resid, sum_out)
-    a = _norm_args(x, resid, gain, eps, sum_out)
-    if a[7]:
-        _check(load().lvx_rmsnorm_residual_fp8(*a, q.data_ptr(), q.stride(0), row_scales.data_ptr(), _stream_of(q)))
-
-
-def _check_like(resid, sum_out):
-    if sum_out is not None and (resid is None or sum_out.dtype != resid.dtype):
-        raise LvxError(1, "the sum has the residual's dtype")
+    found = _norm_args(x, resid, gain, eps, sum_out, q, _e4m3(q))
+    if found is not None:
+        a, device, stream = found
+        _check(load().lvx_rmsnorm_residual_fp8(*a, _vector(row_scales, "row_scales", a[7], device), stream))
 
 
 def lvx_fp4_quantize(x, q=None, scales=None):
     """bf16 [rows][cols] -> (E2M1 codes uint8 [rows][cols / 2], E8M0 scales uint8 [rows][cols / 32])."""
     import torch
     rows, cols = x.shape
+    device, stream = _here_with(x, "x")
     if q is None:
         q = torch.empty((rows, cols // 2), dtype=torch.uint8, device=x.device)
     if scales is None:
         scales = torch.empty((rows, cols // 32), dtype=torch.uint8, device=x.device)
-    _check(load().lvx_fp4_quantize(_ptr(x), x.stride(0), rows, cols, _ptr(q), q.stride(0), _ptr(scales), scales.stride(0), _stream_of(x)))
+    _check(load().lvx_fp4_quantize(*_matrix(x, "x", torch.bfloat16, rows, cols, device), rows, cols, *_matrix(q, "q", torch.uint8, rows, cols // 2, device),
+                                   *_matrix(scales, "scales", torch.uint8, rows, cols // 32, device), stream))
     return q, scales
+
+
+def _fp4_args(M, K, wq, w_scales, c, epi, resid, gate, device):
+    """What the linears with 4-bit weights take behind their rows."""
+    import torch
+    N, half = wq.shape
+    if half * 2 != K or w_scales.shape != (N, K // 32) or K % 32 != 0:
+        raise LvxError(2, f"rows of {K} channels, weights of shape {tuple(wq.shape)} and scales of shape {tuple(w_scales.shape)}: [N][K / 2] and [N][K / 32] are needed")
+    out = torch.float32 if epi == EPI_RESID_GATE_F32 or epi == EPI_STORE_F32 else torch.bfloat16
+    r, ldr = (None, 0) if resid is None else _matrix(resid, "the residual", out, M, N, device)
+    return (*_matrix(wq, "wq", torch.uint8, N, K // 2, device), *_matrix(w_scales, "w_scales", torch.uint8, N, K // 32, device), *_matrix(c, "c", out, M, N, device),
+            M, N, K, epi, r, ldr, _vector(gate, "gate", N, device))
 
 
 def lvx_linear_fp4(a, wq, w_scales, c, epi=EPI_STORE, resid=None, gate=None):
     """c = epilogue(a [M][K] bf16 times the E2M1 weights wq [N][K / 2] with scales [N][K / 32], transposed).  No rows: nothing is done."""
+    import torch
     M, K = a.shape
     if M:
-        _check(load().lvx_linear_fp4(a.data_ptr(), a.stride(0), wq.data_ptr(), wq.stride(0), w_scales.data_ptr(), w_scales.stride(0), c.data_ptr(),
-                                     c.stride(0), M, wq.shape[0], K, epi, _ptr(resid), 0 if resid is None else resid.stride(0), _ptr(gate), _stream_of(c)))
+        device, stream = _here_with(a, "a")
+        _check(load().lvx_linear_fp4(*_matrix(a, "a", torch.bfloat16, M, K, device), *_fp4_args(M, K, wq, w_scales, c, epi, resid, gate, device), stream))
 
 
 def lvx_linear_fp8_fp4(aq, row_scales, wq, w_scales, c, epi=EPI_STORE, resid=None, gate=None):
     """The same for E4M3 rows (uint8 [M][K]) with one fp32 scale each.  epi | EPI_MIXED_8X4 allows many rows the faster 8 x 4-bit products, which cut the small ones of four."""
     M, K = aq.shape
     if M:
-        _check(load().lvx_linear_fp8_fp4(aq.data_ptr(), aq.stride(0), row_scales.data_ptr(), wq.data_ptr(), wq.stride(0), w_scales.data_ptr(),
-                                         w_scales.stride(0), c.data_ptr(), c.stride(0), M, wq.shape[0], K, epi, _ptr(resid),
-                                         0 if resid is None else resid.stride(0), _ptr(gate), _stream_of(c)))
+        device, stream = _here_with(aq, "aq")
+        _check(load().lvx_linear_fp8_fp4(*_matrix(aq, "aq", _e4m3(aq), M, K, device), _vector(row_scales, "row_scales", M, device),
+                                         *_fp4_args(M, K, wq, w_scales, c, epi, resid, gate, device), stream))
 
 
 def kv4_desc(n_layers, n_seqs, n_kv_heads, head_dim, max_keys):
@@ -444,16 +513,27 @@ class KV4Cache:
             pass
 
 
+def _check_cache(cache, device):
+    if cache.storage.get_device() != device:
+        raise LvxError(1, f"the cache lies on {cache.storage.device}, not on the current device")
+
+
 def lvx_kv4_append(cache, layer, k, v, key_counts, starts=None, max_tokens=1, n_tokens=None):
     """k, v: bf16 [n_tokens][kv heads * head_dim] of one row stride; key_counts, starts: device int32."""
-    ld = k.stride(0)
-    if ld != v.stride(0):
-        raise LvxError(2, "k and v must share their row stride")
     n = k.shape[0] if n_tokens is None else n_tokens
     if n:
-        _check(load().lvx_kv4_append(cache.handle, layer, k.data_ptr(), v.data_ptr(), ld,
-                                     None if starts is None else _check_i32(starts, cache.desc.n_seqs + 1, k), n, max_tokens,
-                                     _check_i32(key_counts, cache.desc.n_seqs, k), _stream_of(k)))
+        import torch
+        d = cache.desc
+        n_seqs, width = d.n_seqs, d.n_kv_heads * d.head_dim
+        starts = None if starts is None else _check_i32(starts, n_seqs + 1, k)
+        counts = _check_i32(key_counts, n_seqs, k)
+        device, stream = _here_with(k, "k")
+        k, ld = _matrix(k, "k", torch.bfloat16, n, width, device)
+        v, ld_v = _matrix(v, "v", torch.bfloat16, n, width, device)
+        if ld != ld_v:
+            raise LvxError(2, "k and v must share their row stride")
+        _check_cache(cache, device)
+        _check(load().lvx_kv4_append(cache.handle, layer, k, v, ld, starts, n, max_tokens, counts, stream))
 
 
 def lvx_kv4_gather(cache, layer, key_counts, k_out, v_out, first_key=0):
@@ -462,9 +542,18 @@ def lvx_kv4_gather(cache, layer, key_counts, k_out, v_out, first_key=0):
         if t.dim() != 3 or t.shape[0] != cache.desc.n_seqs or t.shape != k_out.shape or t.stride() != k_out.stride() or (
                 t.shape[0] > 1 and t.shape[1] > 0 and t.stride(0) != t.shape[1] * t.stride(1)):
             raise LvxError(2, "the outputs are [n_seqs][n_keys][columns] of the same strides")
-    if k_out.shape[1]:
-        _check(load().lvx_kv4_gather(cache.handle, layer, first_key, k_out.shape[1], _check_i32(key_counts, cache.desc.n_seqs, k_out), _ptr(k_out), _ptr(v_out),
-                                     k_out.stride(1), _stream_of(k_out)))
+    n = k_out.shape[1]
+    if n:
+        import torch
+        d = cache.desc
+        counts = _check_i32(key_counts, d.n_seqs, k_out)
+        device, stream = _here_with(k_out, "k_out")
+        if v_out.get_device() != device or k_out.dtype is not torch.bfloat16 or v_out.dtype is not torch.bfloat16:
+            raise LvxError(1, "the outputs are bf16 on the current device")
+        if k_out.shape[2] < d.n_kv_heads * d.head_dim or k_out.stride(2) != 1:
+            raise LvxError(2, f"the outputs' rows hold {d.n_kv_heads * d.head_dim} neighbouring elements")
+        _check_cache(cache, device)
+        _check(load().lvx_kv4_gather(cache.handle, layer, first_key, n, counts, k_out.data_ptr(), v_out.data_ptr(), k_out.stride(1), stream))
 
 
 def lvx_kv4_attention_workspace_bytes(cache, n_heads, max_tokens):
@@ -478,10 +567,19 @@ def lvx_kv4_attention(cache, layer, q, n_heads, scale, key_counts, out, workspac
     """q, out: bf16 [n_tokens][heads * head_dim] (no tokens: nothing is done); workspace: lvx_kv4_attention_workspace_bytes(cache, n_heads, max_tokens) bytes."""
     n = q.shape[0] if n_tokens is None else n_tokens
     if n:
-        _check(load().lvx_kv4_attention(cache.handle, layer, q.data_ptr(), q.stride(0), n_heads,
-                                        None if starts is None else _check_i32(starts, cache.desc.n_seqs + 1, q), n, max_tokens,
-                                        _check_i32(key_counts, cache.desc.n_seqs, q), 1 if causal else 0, scale, out.data_ptr(), out.stride(0),
-                                        workspace.data_ptr(), workspace.nbytes, _stream_of(q)))
+        import torch
+        d = cache.desc
+        n_seqs, width = d.n_seqs, n_heads * d.head_dim
+        starts = None if starts is None else _check_i32(starts, n_seqs + 1, q)
+        counts = _check_i32(key_counts, n_seqs, q)
+        device, stream = _here_with(q, "q")
+        q, ld_q = _matrix(q, "q", torch.bfloat16, n, width, device)
+        out, ld_out = _matrix(out, "out", torch.bfloat16, n, width, device)
+        if workspace.get_device() != device or not workspace.is_contiguous():
+            raise LvxError(1, f"the workspace lies on {workspace.device}, not on the current device, or has gaps")
+        _check_cache(cache, device)
+        _check(load().lvx_kv4_attention(cache.handle, layer, q, ld_q, n_heads, starts, n, max_tokens, counts, 1 if causal else 0, scale, out, ld_out,
+                                        workspace.data_ptr(), workspace.nbytes, stream))
 
 
 class StageHandle:
