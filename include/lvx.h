@@ -298,7 +298,7 @@ lvx_status_t lvx_fp4_quantize(const void *dev_x, int64_t ld, int32_t rows, int32
  *   lvx_linear_fp4: A bf16, lda % 8 == 0.   lvx_linear_fp8_fp4: A E4M3 codes with a scale per row, lda in bytes % 16 == 0.  With LVX_EPI_MIXED_8X4 added to an
  *   epilogue of bf16 outputs, more than 32 rows may be multiplied 8 by 4 bits at a higher rate, where products of four neighbouring channels are lined up with the
  *   largest of them and cut 12 binary places below its leading bit; without it every product is exact and the sums are fp32.
- * K % 32 == 0, N % 8 == 0, N <= 2^24, M <= 2^20, ldc, ldr % 8 == 0, ldw in bytes % 16 == 0.  Epilogues STORE, GELU_TANH, RESID_GATE, RESID_GATE_F32, STORE_F32; C may alias R.
+ * K % 32 == 0, K <= 2^30, N % 8 == 0, N <= 2^24, M <= 2^20, ldc, ldr % 8 == 0, ldw in bytes % 16 == 0.  Epilogues STORE, GELU_TANH, RESID_GATE, RESID_GATE_F32, STORE_F32; C may alias R.
  * The same call gives the same bits; the order of summation depends on M, N and K. */
 lvx_status_t lvx_linear_fp4(const void *dev_a, int64_t lda, const void *dev_wq, int64_t ldw, const void *dev_w_scales, int64_t lds, void *dev_c,
                             int64_t ldc, int32_t M, int32_t N, int32_t K, lvx_epilogue_t epi, const void *dev_resid, int64_t ldr,

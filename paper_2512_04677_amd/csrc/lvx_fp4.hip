@@ -651,6 +651,7 @@ lvx_status_t linear(const void *a, int64_t lda, const float *row_scales, bool a8
                 LVX_ERR_INVALID_ARG, "pointers must be 16-byte aligned (scales and gate as their type)");
     LVX_REQUIRE(M >= 0 && N > 0 && K > 0, LVX_ERR_SHAPE, "M %d, N %d, K %d", M, N, K);
     LVX_REQUIRE(K % LVX_FP4_GROUP == 0, LVX_ERR_SHAPE, "K %d must be a multiple of %d", K, LVX_FP4_GROUP);
+    LVX_REQUIRE(K <= 1 << 30, LVX_ERR_SHAPE, "K %d is more than 2^30 channels", K);  // steps and units of steps are counted in 32 bits, rounded up
     LVX_REQUIRE(N % 8 == 0 && N <= 1 << 24, LVX_ERR_SHAPE, "N %d must be a multiple of 8, at most 2^24", N);
     LVX_REQUIRE(lda >= K && lda % (a8 ? 16 : 8) == 0 && ldw >= K / 2 && ldw % 16 == 0 && lds >= K / LVX_FP4_GROUP && ldc >= N && ldc % 8 == 0,
                 LVX_ERR_SHAPE, "bad leading dimension");

@@ -180,3 +180,10 @@ def test_mixed_products_are_for_8bit_rows_and_bf16_outputs():
     for epi in (lvx.EPI_RESID_GATE_F32, lvx.EPI_STORE_F32, lvx.EPI_BIAS, lvx.EPI_BIAS_SILU, 7, 16):
         assert lib.lvx_linear_fp8_fp4(*a8, epi | flag, P, 16, None, None) == (0 if epi == 16 else 1)
     assert lib.lvx_linear(P, 64, P, 64, P, 16, 8, 16, 64, flag, None, 0, None, None) == 1
+
+
+@pytest.mark.parametrize("K,status", [(1 << 30, 0), ((1 << 30) + 32, 2), ((1 << 31) - 256, 2), ((1 << 31) - 32, 2)])
+def test_more_channels_than_the_kernels_count(K, status):
+    lib, ld = lvx.load(), 1 << 31
+    assert lib.lvx_linear_fp4(P, ld, P, ld, P, ld, P, 16, 0, 16, K, 0, None, 0, None, None) == status
+    assert lib.lvx_linear_fp8_fp4(P, ld, P, P, ld, P, ld, P, 16, 0, 16, K, 0, None, 0, None, None) == status
