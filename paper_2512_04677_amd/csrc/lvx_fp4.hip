@@ -602,7 +602,7 @@ void launch_tile_8(const fp4_args_t &p, int blocks, bool four, hipStream_t strea
         blocks == 3 ? launch_tile<MODE, 3, 2, 3>(p, stream) : blocks == 2 ? launch_tile<MODE, 2, 2, 3>(p, stream) : launch_tile<MODE, 1, 2, 3>(p, stream);
 }
 
-// Few rows.  More columns to a workgroup share the loads of A; that pays where enough workgroups are left (16 8-bit rows x 5120 x 5120: two blocks of
+// Few rows, or many that lie too far apart for the tiles.  More columns to a workgroup share the loads of A; that pays where enough workgroups are left (16 8-bit rows x 5120 x 5120: two blocks of
 // columns are fastest, 8.4 us; 16 bf16 rows x 13824 x 5120: 14.3 with four, 17.5 with two; 1280 columns: one).
 template <int MODE>
 void linear_few(const fp4_args_t &p, hipStream_t stream) {
@@ -628,8 +628,8 @@ void linear_launch(const fp4_args_t &p, bool a8, bool mixed, hipStream_t stream)
     // (544 x 5120 x 13824: 51 us against 84): it lines the products of four neighbouring channels up with the largest of them and cuts what lies 12 binary places below
     // its leading bit (measured; the fours and the steps are added in fp32), on normal rows 4e-6 of a sum.  Up to 32 rows are bound by the weights and are widened all the same.
     const int mode = !a8 ? A_BF16 : mixed && p.M > 32 ? A_NATIVE : A_WIDEN;
-    const lvx_fp4_plan_t pl = lvx_fp4_plan(mode, p.M, p.N, p.K);
-    if (pl.blocks == 0 || p.lda >= 1 << 24 || p.ldw >= 1 << 24) {  // tiles reach their rows with 32-bit offsets
+    const lvx_fp4_plan_t pl = lvx_fp4_call_plan(mode, p.M, p.N, p.K, p.lda, p.ldw);
+    if (pl.blocks == 0) {
         a8 ? linear_few<A_WIDEN>(p, stream) : linear_few<A_BF16>(p, stream);
         return;
     }

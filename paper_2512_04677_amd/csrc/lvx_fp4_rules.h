@@ -36,6 +36,14 @@ static inline lvx_fp4_plan_t lvx_fp4_plan(int mode, int M, int N, int K) {
     return best;
 }
 
+// Tiles reach their rows (96 at most) and columns (128) with 32-bit offsets in bytes: below 2^24 bytes a row these stay below 2^31.
+static inline bool lvx_fp4_tiles_reach(int64_t lda, int64_t ldw) { return lda < 1 << 24 && ldw < 1 << 24; }
+
+// The kernel of a call with rows lda and weights ldw bytes apart; further apart, any number of rows goes through the kernels for few.
+static inline lvx_fp4_plan_t lvx_fp4_call_plan(int mode, int M, int N, int K, int64_t lda, int64_t ldw) {
+    return lvx_fp4_tiles_reach(lda, ldw) ? lvx_fp4_plan(mode, M, N, K) : lvx_fp4_plan_t{0, 0};
+}
+
 // Rows that lie in LDS whole, of K values of `bytes` bytes, beside the scales of 16 nb columns.
 static inline int64_t lvx_fp4_resident_bytes(int bytes, int M, int K, int nb) { return (int64_t)M * ((int64_t)K * bytes + 16) + 16 * nb * (((K / 32 + 15) & ~15) + 4); }
 

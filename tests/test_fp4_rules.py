@@ -73,3 +73,20 @@ def test_rows_in_lds(plan):
                     nb = so.resident(bytes_, M, N, K)
                     # never more than a compute unit's LDS
                     assert nb == 0 or (M <= 16 and so.resident_bytes(bytes_, M, K, nb) <= 160 * 1024)
+
+
+def test_rows_far_apart_take_no_tile(plan, tmp_path):
+    (tmp_path / "call.cpp").write_text('#include "lvx_fp4_rules.h"\nextern "C" int blocks(int mode, int M, int N, int K, long long lda, long long ldw) '
+                                       "{ return lvx_fp4_call_plan(mode, M, N, K, lda, ldw).blocks; }\n")
+    lib = str(tmp_path / "libcall.so")
+    subprocess.check_call([shutil.which("g++"), "-O1", "-std=c++17", "-shared", "-fPIC", "-I" + CSRC, str(tmp_path / "call.cpp"), "-o", lib])
+    blocks = C.CDLL(lib).blocks
+    blocks.argtypes = [C.c_int] * 4 + [C.c_longlong] * 2
+    far, near = 1 << 24, (1 << 24) - 16
+    for mode in (BF16, WIDEN, NATIVE):
+        for M, N, K, *_ in gpu_tests.FAR_APART:
+            assert blocks(mode, M, N, K, near, near) > 0 and blocks(mode, M, N, K, far, near) == 0 and blocks(mode, M, N, K, near, far) == 0
+    # the largest offset of a tile: its last row or column, and the bytes of that
+    assert 96 * near < 1 << 32 and 128 * near < 1 << 32
+    # more than three blocks of rows beside few and many columns
+    assert {(-(-M // 16) > 3, N >= 4096) for M, N, *_ in gpu_tests.FAR_APART} >= {(True, False), (True, True)}

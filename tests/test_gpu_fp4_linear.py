@@ -299,3 +299,35 @@ def test_mixed_products_keep_what_is_not_finite(lvx):
     bad[:, 7] = bad[:, 5000] = True
     bad[33] = True
     assert torch.equal(torch.isnan(out), bad)
+
+
+# products that tiles would take; bytes from row to row, from weight to weight beyond their own, which 32-bit offsets do not reach
+FAR_APART = [(50, 4104, 288, 1 << 24, 0), (70, 4104, 160, 1 << 24, 0), (4400, 72, 160, 0, 1 << 24)]
+
+
+@pytest.mark.parametrize("a8", [False, True])
+@pytest.mark.parametrize("M,N,K,lda,ldw", FAR_APART)
+def test_rows_far_apart(lvx, M, N, K, lda, ldw, a8):
+    q, s, w = weights(lvx, N, K, "far")
+    if ldw:
+        wide = torch.empty(N, ldw, dtype=torch.uint8, device=DEV)
+        wide[:, :K // 2] = q
+        q = wide[:, :K // 2]
+    if a8:
+        x, sa, a = rows8(M, K, "far")
+    else:
+        x = S.randn_bf16((M, K), S.seed_of("far", "a", M, K), 1.0, device=DEV)
+        a = S.to_f64(x)
+    if lda:
+        wide_a = torch.empty(M, lda // x.element_size(), dtype=x.dtype, device=DEV)
+        wide_a[:, :K] = x
+        x = wide_a[:, :K]
+    ref, off = a @ w.T, (K + 8) * 2.0 ** -24 * (np.abs(a) @ np.abs(w).T)
+    out, o32 = torch.empty(M, N, dtype=torch.bfloat16, device=DEV), torch.empty(M, N, device=DEV)
+    for c, epi in ((out, lvx.EPI_STORE), (o32, lvx.EPI_STORE_F32)):
+        lvx.lvx_linear_fp8_fp4(x, sa, q, s, c, epi) if a8 else lvx.lvx_linear_fp4(x, q, s, c, epi)
+    assert np.all(np.abs(S.to_f64(o32) - ref) <= off) and torch.equal(out, o32.to(torch.bfloat16))
+    if a8:
+        mixed_out = torch.empty_like(out)
+        lvx.lvx_linear_fp8_fp4(x, sa, q, s, mixed_out, lvx.EPI_STORE | lvx.EPI_MIXED_8X4)
+        assert torch.equal(mixed_out, out)
