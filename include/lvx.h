@@ -294,7 +294,8 @@ lvx_status_t lvx_rmsnorm_residual_fp8(const void *dev_x, int64_t ldx, const void
  * bf16: elements above 1.75 * 2^127).  A group that holds a NaN or an infinity gets scale 255 (NaN).  cols % 32 == 0, ldq >= cols / 2 and % 16 == 0, lds >= cols / 32.  For weights, once. */
 lvx_status_t lvx_fp4_quantize(const void *dev_x, int64_t ld, int32_t rows, int32_t cols, void *dev_q, int64_t ldq, void *dev_scales, int64_t lds,
                               lvx_stream_t stream);
-/* C[M][N] = epilogue(A[M][K] * W[N][K]^T), W in that form (any scale byte; 255 is NaN), fp32 accumulate; for one row as for a prompt.
+/* C[M][N] = epilogue(A[M][K] * W[N][K]^T), W in that form (scale bytes 0 .. 252 exactly; of 253 and 254, weights of 2^128 and
+ * more are infinite, with mixed products perhaps not; 255 is NaN), fp32 accumulate; for one row as for a prompt.
  *   lvx_linear_fp4: A bf16, lda % 8 == 0.   lvx_linear_fp8_fp4: A E4M3 codes with a scale per row, lda in bytes % 16 == 0.  With LVX_EPI_MIXED_8X4 added to an
  *   epilogue of bf16 outputs, more than 32 rows may be multiplied 8 by 4 bits at a higher rate, where products of four neighbouring channels are lined up with the
  *   largest of them and cut 12 binary places below its leading bit; without it every product is exact and the sums are fp32.

@@ -3,7 +3,8 @@
 // Weights and scales are read as they lie ([N][K/2] bytes, [N][K/32] bytes): a matrix instruction sums 128 channels of 16 weight rows, and lane
 // (row r = lane % 16, group g = lane / 16) takes the 16 bytes of channels 32 g .. 32 g + 31 of row r: one scale group, one scale byte, one 16-byte load.
 //
-// Weights stay exact: a code times its scale is a bf16 number, and its products with a bf16 or E4M3 value are exact in fp32.
+// Weights stay exact: below 2^128 (scale bytes up to 252, whatever the code) a code times its scale is a bf16 number, a subnormal one for bytes below 2, which the conversion
+// and the matrix cores keep, and its products with a bf16 or E4M3 value are exact in fp32.
 #include "lvx_fp4.h"
 #include "lvx_fp4_rules.h"
 

@@ -331,3 +331,31 @@ def test_rows_far_apart(lvx, M, N, K, lda, ldw, a8):
         mixed_out = torch.empty_like(out)
         lvx.lvx_linear_fp8_fp4(x, sa, q, s, mixed_out, lvx.EPI_STORE | lvx.EPI_MIXED_8X4)
         assert torch.equal(mixed_out, out)
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 264, 256), (20, 264, 256), (1, 264, 4096), (16, 2056, 4096), (600, 2056, 256), (300, 4104, 160)])
+def test_every_end_of_the_scales(lvx, M, N, K):
+    """One weight a column, all codes and signs, times a power of two: exact from byte 0 (subnormal weights) to 252; from 2^128 on weights are infinite; 255 is NaN."""
+    col = torch.arange(N, device=DEV) % 16
+    q = torch.zeros(N, K // 2, dtype=torch.uint8, device=DEV)
+    q[:, 40] = (col << 4).to(torch.uint8)                # channel 81
+    level = O.e2m1_value(np.arange(N) % 16)
+    for byte in (0, 1, 2, 6, 7, 8, 126, 251, 252, 253, 254, 255):
+        s = torch.full((N, K // 32), byte, dtype=torch.uint8, device=DEV)
+        up = 2.0 ** (100 if byte < 127 else -100)
+        w = level * 2.0 ** (byte - 127)
+        want = np.where(np.abs(w) >= 2.0 ** 128, np.copysign(np.inf, w), w * up) if byte < 255 else np.full(N, np.nan)
+        a = torch.zeros(M, K, dtype=torch.bfloat16, device=DEV)
+        a[:, 81] = up
+        a8, row_scales = torch.zeros(M, K, dtype=torch.uint8, device=DEV), torch.full((M,), up, device=DEV)
+        a8[:, 81] = 0x38                                 # 1
+        c = torch.empty(M, N, device=DEV)
+        lvx.lvx_linear_fp4(a, q, s, c, lvx.EPI_STORE_F32)
+        assert np.array_equal(S.to_f64(c), np.broadcast_to(want, (M, N)), equal_nan=True), byte
+        lvx.lvx_linear_fp8_fp4(a8, row_scales, q, s, c, lvx.EPI_STORE_F32)
+        assert np.array_equal(S.to_f64(c), np.broadcast_to(want, (M, N)), equal_nan=True), byte
+        for epi in (lvx.EPI_STORE, lvx.EPI_STORE | lvx.EPI_MIXED_8X4):
+            out = torch.empty(M, N, dtype=torch.bfloat16, device=DEV)
+            lvx.lvx_linear_fp8_fp4(a8, row_scales, q, s, out, epi)
+            if not (epi & lvx.EPI_MIXED_8X4 and byte in (253, 254)):
+                assert np.array_equal(S.to_f64(out), np.broadcast_to(want, (M, N)), equal_nan=True), (byte, epi)
