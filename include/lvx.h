@@ -275,7 +275,7 @@ lvx_status_t lvx_layernorm_modulate(const void *dev_x, int64_t ldx, const float 
  * from step to step are device arrays, so that a captured step replays with other lengths.
  * ------------------------------------------------------------------------------------------------ */
 
-/* h = x + resid;  y = h / sqrt(mean_c(h^2) + eps) * gain,  fp32 throughout; the norm sees h un-rounded.
+/* h = x + resid;  y = h / sqrt(mean_c(h^2) + eps) * gain,  fp32 throughout (also the sum of the squares, which has to stay below 2^128); the norm sees h un-rounded.
  *   x bf16 or NULL (0); resid bf16, or fp32 with resid_is_f32 = 1 (strides in fp32 elements), or NULL (0), not both NULL; gain fp32 [d] or NULL (1).
  *   dev_sum (may be NULL; needs a residual): h in the residual's type.  dev_y: bf16.  Each output may be the buffer of an input of the same type
  *   and stride.  d % 8 == 0, d <= 16384, strides % 8 == 0, fewer than 2^22 tokens.
@@ -310,7 +310,7 @@ lvx_status_t lvx_linear_fp8_fp4(const void *dev_aq, int64_t lda, const float *de
 
 /* KV cache in 4 bits for n_seqs sequences, grouped heads: head h of the queries reads kv head h / (n_heads / n_kv_heads).  Keys: E2M1 codes with an E8M0
  * scale per key and 32 channels, as lvx_fp4_quantize makes them.  Values: E2M1 codes with one bf16 scale s per key and head, s = bf16(max|v| / 6),
- * at least 2^-120, code = E2M1(v / s).  132 .. 134 bytes per key and kv head of 128 channels.  Storage (caller-owned, 256-byte aligned, alive as long as
+ * at least 2^-120, code = E2M1(v / s).  134 bytes per key and kv head of 128 channels, 68 of 64, for whole tiles of 64 keys.  Storage (caller-owned, 256-byte aligned, alive as long as
  * the handle) need not be cleared; its layout is private.
  *
  * A call handles n_tokens new tokens in all, at most max_tokens of a sequence: sequence s has rows [dev_starts[s], dev_starts[s + 1]) (device int32 [n_seqs + 1];

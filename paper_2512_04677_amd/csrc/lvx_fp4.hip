@@ -21,7 +21,7 @@ struct fp4_args_t {
     int M, N, K, epi;
 };
 
-// 16 E4M3 codes, exact in bf16
+// Eight E4M3 codes, exact in bf16
 __device__ __forceinline__ bf16x8_t fp8x8_bf16(uint32_t lo, uint32_t hi) {
     bf16x8_t r;
     const bf16x2_t a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true);
@@ -258,9 +258,9 @@ __global__ void __launch_bounds__(512) lvx_fp4_few_kernel(fp4_args_t p) {
 }
 
 // ---- rows that fit the LDS ----------------------------------------------------------------------------------------------
-// The same for up to sixteen rows that lie in LDS whole, with the columns' scales beside them, brought there once while the first weights are on their
-// way: the loop then requests nothing but weights, two steps ahead of a wave's own.  One row x 15360 x 5120:
-// 9.4 us, 4.4 TB/s.
+// The same for up to sixteen rows that lie in LDS whole, with the columns' scales beside them: the loop then requests nothing but weights, two steps ahead of a wave's own.
+// Bound by the weights' way once it runs, and by the rows' way before it: they come 16 bytes a thread at a time, each load waited for, and the first weights with it.
+// One row x 15360 x 5120: 9.4 us, 4.4 TB/s.
 template <int MODE, int NB>
 __global__ void __launch_bounds__(512) lvx_fp4_resident_kernel(fp4_args_t p) {
     constexpr int AV = MODE == A_BF16 ? 4 : 2, STEP_A = MODE == A_BF16 ? 256 : 128;
@@ -362,8 +362,8 @@ __global__ void __launch_bounds__(512) lvx_fp4_resident_kernel(fp4_args_t p) {
 // Bound by the matrix cores and the LDS.  Eight waves: KG groups over K, every KG-th pair of steps each, of two waves over the rows and one or two over the columns.  Rows
 // and weights come by direct loads to LDS, RING steps and a pair or two of steps ahead: a stage of the weights is a pair, because a weight row's 128 channels are half a
 // cache line and halves cost as much as lines.  A wave reads the next step's operands into registers while it multiplies this one's.  16-byte chunk c of a row of CH
-// chunks lies at c ^ (row % CH), so that the sixteen rows of an operand fall into different banks.  544 8-bit rows x 5120 x 13824: 52 us, 1.49 PFLOP/s; of that the loop without
-// loads, reads and products is 26, the reads of LDS 16, the products 19, and they overlap only in part.
+// chunks lies at c ^ (row % CH): the sixteen rows of an operand fall into different banks where a row has 256 bytes; of 128-byte rows those eight apart share theirs, and
+// conflicts are more than half of the LDS's cycles.  544 8-bit rows x 5120 x 13824: 84 to 88 us, 0.9 PFLOP/s, the matrix cores busy for a third of it; with mixed products 51 to 53, 1.5.
 template <int MODE, int MBW, int KG, int RING>
 __global__ void __launch_bounds__(512) lvx_fp4_tile_kernel(fp4_args_t p) {
     constexpr int NB = 4, AV = MODE == A_BF16 ? 4 : 2, ROW = MODE == A_BF16 ? 256 : 128, CH = ROW / 16, MT = 32 * MBW;

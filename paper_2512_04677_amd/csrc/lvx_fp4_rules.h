@@ -11,7 +11,7 @@ struct lvx_fp4_plan_t {
 
 // Tiles pay from some product of rows (in blocks of 16) and columns on, later where the rows are few or have to be widened: 64 x 5120 x 5120 15, 14 and 10 us (bf16, widened,
 // mixed) against 30, 19 and 19 of the few-row kernels, 64 x 1280 x 1280 6.7, 6.9 and 5.7 against 8.7, 6.5 and 6.5; but 40 x 2568 x 1184 7.0, 7.1 and 5.9 against 6.0,
-// 5.3 and 5.3, and 24 x 5120 x 13824 36 and 34 against 34 and 25 (bf16, widened).
+// 5.3 and 5.3, and 24 x 5120 x 13824 36 and 34 against 34 and 25 (bf16, widened; mixed products are taken where the caller asks for them).
 // Of the tiles the one that takes the least time: rounds of one workgroup a compute unit, of a start and a time per step of 128 channels that were measured in one round.  Four
 // groups over K have half the columns and half the steps one after the other: where two leave units idle they are faster (64 x 5120 x 13824 54 -> 38 us and, mixed, 35 -> 22).
 static inline lvx_fp4_plan_t lvx_fp4_plan(int mode, int M, int N, int K) {

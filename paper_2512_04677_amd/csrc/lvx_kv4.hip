@@ -10,7 +10,7 @@
 //           second product sums over keys, so a scale of V can neither wait until after it nor, unless a power of two, go into its operand without rounding).
 //
 // One token each of 32 sequences of up to 24960 keys (8 kv heads, 40 heads, 510 MB): 91 us with the join, 5.6 TB/s, bound by HBM.  1560 tokens of 40 heads against 24960 keys:
-// 734 to 753 us on different cards, 1.05 PFLOP/s, bound by the vector unit (conversions, exponentials, packing: about 340 instructions a wave and tile beside 64 matrix products).
+// 730 to 780 us on different cards, 1.0 to 1.06 PFLOP/s, bound by the vector unit (conversions, exponentials, packing: about 350 instructions a wave and tile beside 64 matrix products).
 #include "lvx_fp4.h"
 #include "lvx_kv4_rules.h"
 
@@ -416,7 +416,9 @@ __global__ void __launch_bounds__(64 * WR * WK, 2) lvx_kv4_attention_kernel(attn
             };
             // The reference that is subtracted only has to keep the powers inside fp32.  With the running maximum the largest probability is 1 and its rounding exact, which
             // peaked rows notice (errors of 1.7e-3 against 2.1e-3 with a reference that lags by up to 2^20): where the cache's bytes bound the kernel, that is what it is.
-            // Where the vector unit does (one wave per tile of keys), it is the first tile's maximum, and a tile whose powers reach 2^4 of it moves it (1.9e-3).
+            // Where the vector unit does (one wave per tile of keys), it is the first tile's maximum, and a tile whose powers reach 2^4 of it moves it.  A power rounds to bf16 by
+            // the same share of itself wherever the reference lies; only one of exactly 1 does not round (outputs 2.25e-3 off against 2.12e-3 with the running maximum, which
+            // takes 763 us for 731).
             // A row whose scores so far are all -infinity takes its reference from the next tile, above zero or below.
             constexpr bool RUNNING = WK > 1;
             bool move = unset[b];

@@ -10,9 +10,10 @@ struct lvx_kv4_plan_t {
     int rows, row_tiles, splits;  // rows of a workgroup (tokens x heads of a group): 16, 32, 64 or 128; workgroups a sequence and kv head; ranges of keys
 };
 
-// The form and the ranges with the least time by the measured time of an iteration (head_dim 128): a workgroup goes through its range of keys `waves` tiles of 64 at a time,
+// The form and the ranges with the least time by the measured time of an iteration (head_dim 128; 64 takes the same constants, unmeasured): a workgroup goes through its range of keys `waves` tiles of 64 at a time,
 // in 0.1 us `alone` on its compute unit or `beside` a second one, and 512 of them take `full`.  Few rows to a workgroup fill the chip from fewer rows, many read the keys
-// less often: 64 tokens of 40 heads against 1560 keys 9.6 us in blocks of 16 rows, 51 of 128; 1560 tokens against 24960 keys 734 us in 128.  A causal prompt's
+// less often: 64 tokens of 40 heads against 1560 keys 9.6 us in blocks of 16 rows, 51 of 128 (a cache of as many places: the rule knows those, not the keys that there
+// are, and with 24960 places takes another form, 14.0 us); 1560 tokens against 24960 keys 734 us in 128.  A causal prompt's
 // workgroups see fewer keys the earlier their rows: where there are more than stay at once, they cost the average, the longest bounds the others.  Ranges cost the launch
 // that joins them, 5 us and the partial outputs' way out and in: one token of 40 heads against 4680 keys 9.3 us in twelve, 18.6 in one; 512 tokens of 8 heads against
 // 4096 keys 18.0 in one, 25.9 in two.
