@@ -181,15 +181,21 @@ def _here_with(t, what):
     raise LvxError(1, f"{what} lies on {t.device}, not on the current device")
 
 
-def _matrix(t, what, dtype, rows, cols, device):
-    """Address and row stride of a tensor that the library takes as [rows][cols] of dtype: what the kernel would read or write has to be there."""
+def _matrix(t, what, dtype, rows, cols, device, same=None):
+    """Address and row stride of a tensor that the library takes as [rows][cols] of dtype: what the kernel would read or write has to be there.
+    A row may be several dimensions without gaps between them (heads and channels); bytes may be of torch's type of the name `same`."""
     try:
         r, c = t.shape
         ld, step = t.stride()
         if r >= rows and c >= cols and t.dtype is dtype and t.get_device() == device and (step == 1 or cols < 2):
             return t.data_ptr(), ld
     except ValueError:  # not two dimensions
-        pass
+        if t.dim() > 2 and t.flatten(1).data_ptr() == t.data_ptr():
+            return _matrix(t.flatten(1), what, dtype, rows, cols, device)
+    if same is not None:
+        import torch
+        if t.dtype is getattr(torch, same, None):
+            return _matrix(t, what, t.dtype, rows, cols, device)
     if t.get_device() != device:
         raise LvxError(1, f"{what} lies on {t.device}, not on the current device")
     if t.dtype is not dtype:
@@ -205,12 +211,6 @@ def _vector(t, what, n, device):
     if t.get_device() == device and t.dtype is torch.float32 and t.numel() >= n and t.is_contiguous():
         return t.data_ptr()
     raise LvxError(1, f"{what} is a contiguous float32 tensor of at least {n} elements on the current device")
-
-
-def _e4m3(t):
-    """The dtype of E4M3 codes: uint8, or torch's own."""
-    import torch
-    return torch.float8_e4m3fn if t.dtype is torch.float8_e4m3fn else torch.uint8
 
 
 def _check_i32(t, n, like):
@@ -396,7 +396,7 @@ def lvx_layernorm_modulate(x, shift, scale, eps, u):
                                          _ptr(u), u.stride(0), _stream()))
 
 
-def _norm_args(x, resid, gain, eps, sum_out, y, y_type):
+def _norm_args(x, resid, gain, eps, sum_out, y, y_type, y_same=None):
     """The norms' arguments up to y, the device and the stream; no rows: None."""
     import torch
     like = resid if x is None else x
@@ -418,7 +418,7 @@ def _norm_args(x, resid, gain, eps, sum_out, y, y_type):
         r, ldr = _matrix(resid, "the residual", torch.float32 if f32 else torch.bfloat16, n, d, device)
         if sum_out is not None:
             s, ld_sum = _matrix(sum_out, "the sum", torch.float32 if f32 else torch.bfloat16, n, d, device)
-    return (x, ldx, r, ldr, f32, _vector(gain, "gain", d, device), eps, n, d, s, ld_sum, *_matrix(y, "y", y_type, n, d, device)), device, stream
+    return (x, ldx, r, ldr, f32, _vector(gain, "gain", d, device), eps, n, d, s, ld_sum, *_matrix(y, "y", y_type, n, d, device, y_same)), device, stream
 
 
 def lvx_rmsnorm_residual(x, resid, gain, eps, y, sum_out=None):
@@ -432,7 +432,8 @@ def lvx_rmsnorm_residual(x, resid, gain, eps, y, sum_out=None):
 
 def lvx_rmsnorm_residual_fp8(x, resid, gain, eps, q, row_scales, sum_out=None):
     """The same with y as E4M3 codes (uint8 [n][>= d]) and one fp32 scale a row."""
-    found = _norm_args(x, resid, gain, eps, sum_out, q, _e4m3(q))
+    import torch
+    found = _norm_args(x, resid, gain, eps, sum_out, q, torch.uint8, "float8_e4m3fn")
     if found is not None:
         a, device, stream = found
         _check(load().lvx_rmsnorm_residual_fp8(*a, _vector(row_scales, "row_scales", a[7], device), stream))
@@ -447,8 +448,8 @@ def lvx_fp4_quantize(x, q=None, scales=None):
         q = torch.empty((rows, cols // 2), dtype=torch.uint8, device=x.device)
     if scales is None:
         scales = torch.empty((rows, cols // 32), dtype=torch.uint8, device=x.device)
-    _check(load().lvx_fp4_quantize(*_matrix(x, "x", torch.bfloat16, rows, cols, device), rows, cols, *_matrix(q, "q", torch.uint8, rows, cols // 2, device),
-                                   *_matrix(scales, "scales", torch.uint8, rows, cols // 32, device), stream))
+    _check(load().lvx_fp4_quantize(*_matrix(x, "x", torch.bfloat16, rows, cols, device), rows, cols, *_matrix(q, "q", torch.uint8, rows, cols // 2, device, "float4_e2m1fn_x2"),
+                                   *_matrix(scales, "scales", torch.uint8, rows, cols // 32, device, "float8_e8m0fnu"), stream))
     return q, scales
 
 
@@ -460,7 +461,8 @@ def _fp4_args(M, K, wq, w_scales, c, epi, resid, gate, device):
         raise LvxError(2, f"rows of {K} channels, weights of shape {tuple(wq.shape)} and scales of shape {tuple(w_scales.shape)}: [N][K / 2] and [N][K / 32] are needed")
     out = torch.float32 if epi == EPI_RESID_GATE_F32 or epi == EPI_STORE_F32 else torch.bfloat16
     r, ldr = (None, 0) if resid is None else _matrix(resid, "the residual", out, M, N, device)
-    return (*_matrix(wq, "wq", torch.uint8, N, K // 2, device), *_matrix(w_scales, "w_scales", torch.uint8, N, K // 32, device), *_matrix(c, "c", out, M, N, device),
+    return (*_matrix(wq, "wq", torch.uint8, N, K // 2, device, "float4_e2m1fn_x2"), *_matrix(w_scales, "w_scales", torch.uint8, N, K // 32, device, "float8_e8m0fnu"),
+            *_matrix(c, "c", out, M, N, device),
             M, N, K, epi, r, ldr, _vector(gate, "gate", N, device))
 
 
@@ -475,10 +477,11 @@ def lvx_linear_fp4(a, wq, w_scales, c, epi=EPI_STORE, resid=None, gate=None):
 
 def lvx_linear_fp8_fp4(aq, row_scales, wq, w_scales, c, epi=EPI_STORE, resid=None, gate=None):
     """The same for E4M3 rows (uint8 [M][K]) with one fp32 scale each.  epi | EPI_MIXED_8X4 allows many rows the faster 8 x 4-bit products, which cut the small ones of four."""
+    import torch
     M, K = aq.shape
     if M:
         device, stream = _here_with(aq, "aq")
-        _check(load().lvx_linear_fp8_fp4(*_matrix(aq, "aq", _e4m3(aq), M, K, device), _vector(row_scales, "row_scales", M, device),
+        _check(load().lvx_linear_fp8_fp4(*_matrix(aq, "aq", torch.uint8, M, K, device, "float8_e4m3fn"), _vector(row_scales, "row_scales", M, device),
                                          *_fp4_args(M, K, wq, w_scales, c, epi, resid, gate, device), stream))
 
 
@@ -519,7 +522,7 @@ def _check_cache(cache, device):
 
 
 def lvx_kv4_append(cache, layer, k, v, key_counts, starts=None, max_tokens=1, n_tokens=None):
-    """k, v: bf16 [n_tokens][kv heads * head_dim] of one row stride; key_counts, starts: device int32."""
+    """k, v: bf16 [n_tokens][kv heads * head_dim] of one row stride (heads and channels may be two dimensions); key_counts, starts: device int32."""
     n = k.shape[0] if n_tokens is None else n_tokens
     if n:
         import torch
@@ -564,7 +567,7 @@ def lvx_kv4_attention_workspace_bytes(cache, n_heads, max_tokens):
 
 
 def lvx_kv4_attention(cache, layer, q, n_heads, scale, key_counts, out, workspace, starts=None, max_tokens=1, causal=True, n_tokens=None):
-    """q, out: bf16 [n_tokens][heads * head_dim] (no tokens: nothing is done); workspace: lvx_kv4_attention_workspace_bytes(cache, n_heads, max_tokens) bytes."""
+    """q, out: bf16 [n_tokens][heads * head_dim], or [n_tokens][heads][head_dim] (no tokens: nothing is done); workspace: lvx_kv4_attention_workspace_bytes(cache, n_heads, max_tokens) bytes."""
     n = q.shape[0] if n_tokens is None else n_tokens
     if n:
         import torch

@@ -173,3 +173,37 @@ def test_more_tokens_than_rows(stub):
     with pytest.raises(lvx.LvxError):
         lvx.lvx_kv4_attention(Cache(), 0, t["q"], 6, 0.1, t["counts"], t["out"], t["workspace"], starts=t["starts"], n_tokens=M)
     assert not stub.calls
+
+
+def test_heads_as_a_dimension(stub):
+    """[tokens][heads][channels] is the same memory as [tokens][heads * channels] where it has no gaps inside a token."""
+    c = calls()["append"][1]
+    k, v = torch.zeros(M, 2, 64, dtype=BF), torch.zeros(M, 2, 64, dtype=BF)
+    counts, starts = On(c["counts"]), On(c["starts"])
+    lvx.lvx_kv4_append(Cache(), 0, On3(k), On3(v), counts, starts=starts)
+    q, out = torch.zeros(M, 6, 64, dtype=BF)[:, :4], torch.zeros(M, 4, 64, dtype=BF)
+    lvx.lvx_kv4_attention(Cache(), 0, On3(q), 4, 0.1, counts, On3(out), On(torch.zeros(256, dtype=U8)), starts=starts)
+    assert [a[2:5] for _, a in stub.calls] == [(k.data_ptr(), v.data_ptr(), 128), (q.data_ptr(), 384, 4)]
+    stub.calls.clear()
+    for bad in (torch.zeros(M, 2, 72, dtype=BF)[:, :, :64], torch.zeros(M, 64, 2, dtype=BF).transpose(1, 2), torch.zeros(2, M, 64, dtype=BF).transpose(0, 1), k[0]):
+        with pytest.raises(lvx.LvxError):
+            lvx.lvx_kv4_append(Cache(), 0, On3(k), On3(bad), counts, starts=starts, n_tokens=M)
+    assert not stub.calls
+
+
+class On3(On):
+    def flatten(self, first):
+        return On(self.t.flatten(first))
+
+
+def test_bytes_by_their_torch_types(stub):
+    w, s = torch.zeros(N, K // 2, dtype=U8), torch.zeros(N, K // 32, dtype=U8)
+    for name, t in (("float4_e2m1fn_x2", "w"), ("float8_e8m0fnu", "s")):
+        dtype = getattr(torch, name, None)
+        if dtype is None:
+            continue
+        f = lambda x, which: On(x.view(dtype)) if t == which else On(x)
+        lvx.lvx_linear_fp4(On(rows(M, K)), f(w, "w"), f(s, "s"), On(rows(M, N)))
+        lvx.lvx_fp4_quantize(On(rows(N, K)), f(w, "w"), f(s, "s"))
+    lvx.lvx_rmsnorm_residual_fp8(On(rows(M, K)), None, None, 1e-6, On(torch.zeros(M, K, dtype=U8).view(torch.float8_e4m3fn)), On(torch.zeros(M)))
+    assert len(stub.calls) == 1 + 2 * sum(hasattr(torch, n) for n in ("float4_e2m1fn_x2", "float8_e8m0fnu"))
